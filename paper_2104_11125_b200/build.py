@@ -12,15 +12,17 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libscalecom.so")
 STAMP = LIB + ".srchash"
 
-SOURCES = ["scalecom.cu", "topk_static.cu"]
-HEADERS = ["common.cuh", "topk_select.cuh", "learner_pass.cuh", "chunk_select.cuh", "diagnostics.cuh", "exchange.cuh", "layer_topk.cuh", "small_step.cuh"]
+SOURCES = ["scalecom.cu", "topk_static.cu", "operators.cu"]
+HEADERS = ["common.cuh", "topk_select.cuh", "learner_pass.cuh", "chunk_select.cuh", "diagnostics.cuh", "exchange.cuh", "layer_topk.cuh", "small_step.cuh",
+           "ops_common.cuh", "layer_norm.cuh", "operand_prep.cuh", "tc_product.cuh"]
+API_HEADERS = ["scalecom.h", "scalecom_operators.h"]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17",
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-lineinfo",
     "-Xcompiler", "-fPIC", "-shared",
-    "-cudart", "static",
+    "-cudart", "static", "--threads", "4",
 ]
 
 
@@ -36,8 +38,9 @@ def source_hash() -> str:
     for name in SOURCES + HEADERS:
         with open(os.path.join(CSRC, name), "rb") as f:
             h.update(f.read())
-    with open(os.path.join(INCLUDE, "scalecom.h"), "rb") as f:
-        h.update(f.read())
+    for name in API_HEADERS:
+        with open(os.path.join(INCLUDE, name), "rb") as f:
+            h.update(f.read())
     return h.hexdigest()
 
 

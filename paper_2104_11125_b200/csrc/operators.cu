@@ -1,0 +1,882 @@
+// C-ABI of the learner-side operators (see include/scalecom_operators.h): argument checks, scratch, launches.
+#include "../../include/scalecom_operators.h"
+
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "layer_norm.cuh"
+#include "operand_prep.cuh"
+#include "ops_common.cuh"
+#include "tc_product.cuh"
+
+using namespace sc;
+
+struct scalecom_ops {
+    int device = 0;
+    int sms = 0;
+    cudaStream_t stream = nullptr;
+    void* ws = nullptr;                 // scratch of the calls, grown on demand
+    size_t ws_bytes = 0;
+    uint32_t* ctrl = nullptr;           // device: [0] status, [16..] arrival counters of split products
+    PFN_cuTensorMapEncodeTiled encode = nullptr;
+    bool poisoned = false;
+};
+
+namespace {
+
+constexpr int CTRL_WORDS = 16 + 4096;
+constexpr int MAX_SPLIT_TILES = 4096;
+
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev) {
+        if (cudaGetDevice(&prev) != cudaSuccess) return;
+        ok = (prev == dev) || (cudaSetDevice(dev) == cudaSuccess);
+    }
+    ~DeviceGuard() {
+        int cur = -1;
+        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
+    }
+};
+
+inline int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline bool type_ok(int t) { return t == SCALECOM_F32 || t == SCALECOM_F16 || t == SCALECOM_BF16; }
+inline int64_t type_size(int t) { return t == SCALECOM_F32 ? 4 : 2; }
+inline bool dim_ok(int64_t v, int64_t low) { return v >= low && v <= SCALECOM_OPS_MAX_DIM; }
+
+int ensure_ws(scalecom_ops* o, size_t bytes) {
+    if (bytes <= o->ws_bytes) return SCALECOM_OK;
+    if (cudaStreamSynchronize(o->stream) != cudaSuccess) return SCALECOM_ERR_CUDA;
+    cudaFree(o->ws);
+    o->ws = nullptr;
+    o->ws_bytes = 0;
+    if (cudaMalloc(&o->ws, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return SCALECOM_ERR_ALLOC;
+    }
+    o->ws_bytes = bytes;
+    return SCALECOM_OK;
+}
+
+// Scratch is laid out in two passes of the same code: the first (base NULL) counts, the second hands out addresses.
+struct Carver {
+    char* base;
+    size_t used = 0;
+    template <typename T> T* take(int64_t count) {
+        T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+        used = (used + size_t(count) * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+template <typename... A, typename... B>
+cudaError_t launch(scalecom_ops* o, void (*kernel)(A...), dim3 grid, int threads, size_t smem, B&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = o->stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<A>(args)...);
+}
+
+int enter(scalecom_ops* o) { return !o ? SCALECOM_ERR_NULL_PTR : o->poisoned ? SCALECOM_ERR_BAD_STATE : SCALECOM_OK; }
+
+// ---- layer norm --------------------------------------------------------------------------------------------
+template <typename T, int VEC, int NV, int TPR>
+cudaError_t ln_launch(scalecom_ops* o, const LnParams& P) {
+    const int64_t want = ceil_div(P.rows, LN_THREADS / TPR), cap = int64_t(o->sms) * 8;
+    return launch(o, layer_norm_kernel<T, VEC, NV, TPR>, dim3(unsigned(want < cap ? want : cap)), LN_THREADS, 0, P);
+}
+template <typename T, int VEC>
+cudaError_t ln_forward(scalecom_ops* o, const LnParams& P) {
+    const int w = P.width;
+    constexpr int W = 32 * VEC, B = LN_THREADS * VEC;
+    if (w <= W) return ln_launch<T, VEC, 1, 32>(o, P);
+    if (w <= 2 * W) return ln_launch<T, VEC, 2, 32>(o, P);
+    if (w <= 4 * W) return ln_launch<T, VEC, 4, 32>(o, P);
+    if (w <= B) return ln_launch<T, VEC, 1, LN_THREADS>(o, P);
+    if (w <= 2 * B) return ln_launch<T, VEC, 2, LN_THREADS>(o, P);
+    if (w <= 4 * B) return ln_launch<T, VEC, 4, LN_THREADS>(o, P);
+    if (VEC == 1 && w <= 16 * B) return ln_launch<T, VEC, VEC == 1 ? 16 : 1, LN_THREADS>(o, P);
+    const int64_t cap = int64_t(o->sms) * 8;
+    return launch(o, layer_norm_wide_kernel<T>, dim3(unsigned(P.rows < cap ? P.rows : cap)), LN_THREADS, 0, P);
+}
+template <typename T>
+cudaError_t ln_forward_t(scalecom_ops* o, const LnParams& P) {
+    constexpr int V = 16 / sizeof(T);
+    const bool vec = ((reinterpret_cast<uintptr_t>(P.x) | reinterpret_cast<uintptr_t>(P.y)) & 15u) == 0 && P.ldx % V == 0 && P.ldy % V == 0;
+    return vec ? ln_forward<T, V>(o, P) : ln_forward<T, 1>(o, P);
+}
+
+// the backward pass keeps two sums a column in registers, so its rows leave the registers earlier
+template <typename T, int VEC, int NV, int TPR>
+cudaError_t ln_launch_backward(scalecom_ops* o, LnParams& P) {
+    const int64_t want = ceil_div(P.rows, LN_THREADS / TPR), cap = int64_t(o->sms) * 2;
+    P.nblocks = int32_t(want < cap ? want : cap);
+    const size_t smem = TPR == 32 ? size_t(P.width) * 8 : 0;
+    if (P.dgamma || P.dbeta)
+        return launch(o, layer_norm_backward_kernel<T, VEC, NV, TPR, true>, dim3(P.nblocks), LN_THREADS, smem, P);
+    return launch(o, layer_norm_backward_kernel<T, VEC, NV, TPR, false>, dim3(P.nblocks), LN_THREADS, 0, P);
+}
+template <typename T, int VEC>
+cudaError_t ln_backward(scalecom_ops* o, LnParams& P) {
+    const int w = P.width;
+    constexpr int W = 32 * VEC, B = LN_THREADS * VEC;
+    if (w <= W) return ln_launch_backward<T, VEC, 1, 32>(o, P);
+    if (w <= 2 * W) return ln_launch_backward<T, VEC, 2, 32>(o, P);
+    if (w <= 4 * W) return ln_launch_backward<T, VEC, 4, 32>(o, P);
+    if (w <= B) return ln_launch_backward<T, VEC, 1, LN_THREADS>(o, P);
+    if (w <= 2 * B) return ln_launch_backward<T, VEC, 2, LN_THREADS>(o, P);
+    if (w <= 4 * B) return ln_launch_backward<T, VEC, 4, LN_THREADS>(o, P);
+    if (VEC <= 4 && w <= 8 * B) return ln_launch_backward<T, VEC, VEC <= 4 ? 8 : 1, LN_THREADS>(o, P);
+    if (VEC == 1 && w <= 16 * B) return ln_launch_backward<T, VEC, VEC == 1 ? 16 : 1, LN_THREADS>(o, P);
+    if (P.dgamma || P.dbeta) {                            // before dx, which may overwrite dy
+        const int64_t cols = ceil_div(w, LN_THREADS);
+        int64_t groups = ceil_div(int64_t(o->sms) * 8, cols);
+        if (groups > P.rows) groups = P.rows;
+        if (groups > o->sms * 2) groups = o->sms * 2;
+        P.nblocks = int32_t(groups);
+        const cudaError_t e = launch(o, layer_norm_columns_kernel<T>, dim3(unsigned(cols), unsigned(groups)), LN_THREADS, 0, P);
+        if (e != cudaSuccess) return e;
+    }
+    if (!P.dx) return cudaSuccess;
+    const int64_t cap = int64_t(o->sms) * 8;
+    return launch(o, layer_norm_backward_wide_kernel<T>, dim3(unsigned(P.rows < cap ? P.rows : cap)), LN_THREADS, 0, P);
+}
+template <typename T>
+cudaError_t ln_backward_t(scalecom_ops* o, LnParams& P) {
+    constexpr int V = 16 / sizeof(T);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(P.x) | reinterpret_cast<uintptr_t>(P.dy) | reinterpret_cast<uintptr_t>(P.dx);
+    const bool vec = (at & 15u) == 0 && P.ldx % V == 0 && P.lddy % V == 0 && (!P.dx || P.lddx % V == 0);
+    return vec ? ln_backward<T, V>(o, P) : ln_backward<T, 1>(o, P);
+}
+
+// ---- products ------------------------------------------------------------------------------------------------
+// A matrix as the tensor cores read it: [batch][planes][rows][ld], 16-bit, 16-byte aligned rows.
+struct Operand {
+    const void* p = nullptr;
+    int64_t rows = 0, cols = 0, ld = 0;
+    int planes = 1;
+    int64_t plane = 0;             // elements between planes
+    int batch = 1;
+    int64_t stride = 0;            // elements between matrices
+    const uint32_t* amax = nullptr;
+};
+
+inline bool tma_ready(const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0; }
+
+// mn: the operand's own rows are contiguous (its stored columns are m or n, its stored rows k)
+bool encode(scalecom_ops* o, CUtensorMap* map, const Operand& a, bool bf16, bool mn, int box_rows) {
+    const int64_t lead = a.rows * a.ld * 2;
+    cuuint64_t dims[4] = {cuuint64_t(a.cols), cuuint64_t(a.rows), cuuint64_t(a.planes), cuuint64_t(a.batch)};
+    cuuint64_t strides[3] = {cuuint64_t(a.ld * 2), cuuint64_t(a.planes > 1 ? a.plane * 2 : lead),
+                             cuuint64_t(a.batch > 1 ? a.stride * 2 : lead)};
+    cuuint32_t box[4] = {64, cuuint32_t(mn ? TC_BK : box_rows), 1, 1};
+    cuuint32_t el[4] = {1, 1, 1, 1};
+    return o->encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(a.p),
+                     dims, strides, box, el, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Product {
+    const Operand *a = nullptr, *b = nullptr, *a2 = nullptr, *b2 = nullptr;   // second pair: GATE's up weights (b2), or a second product
+    bool a_mn = false, b_mn = false, a_batched = false, b_batched = false, bf16 = false;
+    int64_t m = 0, n = 0, k = 0;
+    int batch = 1;
+};
+
+struct Plan { int bn, splits; int64_t mt, nt, tiles; };
+
+// Tiles and parts of k. A part of one 64-wide block of k costs about 512 cycles of the tensor core with 256-wide tiles and, bound by
+// shared memory and issue, about 320 with 128-wide ones; a split part costs its accumulators' way through L2.
+Plan make_plan(const scalecom_ops* o, int epi, int planes, int64_t m, int64_t n, int64_t iters, int64_t batch) {
+    Plan best = {};
+    double least = 1e300;
+    for (int bn = planes > 1 ? 128 : 256; bn >= 128; bn /= 2) {      // two planes: the sums take too many registers for 256
+        Plan p;
+        p.bn = bn;
+        p.mt = ceil_div(m, TC_BM);
+        p.nt = ceil_div(n, epi == EPI_GATE ? bn / 2 : bn);
+        p.tiles = p.mt * p.nt;
+        if (epi == EPI_GRAM || epi == EPI_POLY) {
+            p.tiles = 0;
+            for (int64_t i = 0; i < p.mt; ++i) {
+                const int64_t c = (i * TC_BM + TC_BM - 1) / bn + 1;
+                p.tiles += c < p.nt ? c : p.nt;
+            }
+        }
+        const double block = planes > 1 ? 1000.0 : bn == 256 ? 512.0 : 320.0, drain = bn * 6.0;
+        for (int s = 1; s <= 32 && (s == 1 || s * 2 <= iters); ++s) {
+            if (s > 1 && p.tiles * batch > MAX_SPLIT_TILES) break;
+            const double waves = double(ceil_div(p.tiles * batch * s, o->sms));
+            const double cost = waves * double(ceil_div(iters, s)) * block + drain + (s > 1 ? (waves + s) * bn * 5.0 + 2000.0 : 0.0);
+            if (cost < least * 0.97) {
+                least = cost;
+                best = p;
+                best.splits = s;
+            }
+        }
+    }
+    return best;
+}
+
+int64_t product_iters(const Product& p) {
+    return ceil_div(p.k, TC_BK) * (p.a2 ? 2 : 1);
+}
+
+template <int BN, int EPI, int PL>
+cudaError_t tc_launch(scalecom_ops* o, const TcParams& P) {
+    const int64_t units = int64_t(P.batch) * P.tiles * P.splits;
+    return launch(o, tc_product_kernel<BN, EPI, PL>, dim3(unsigned(units < o->sms ? units : o->sms)), TC_THREADS, TcShape<BN, PL>::SMEM, P);
+}
+template <int EPI>
+cudaError_t tc_launch_any(scalecom_ops* o, int bn, int planes, const TcParams& P) {
+    if (planes > 1) return tc_launch<128, EPI, 2>(o, P);
+    return bn == 256 ? tc_launch<256, EPI, 1>(o, P) : tc_launch<128, EPI, 1>(o, P);
+}
+template <int EPI>
+cudaError_t tc_attributes() {
+    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    cudaError_t e = cudaFuncSetAttribute(tc_product_kernel<256, EPI, 1>, attr, TcShape<256, 1>::SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_product_kernel<128, EPI, 1>, attr, TcShape<128, 1>::SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_product_kernel<128, EPI, 2>, attr, TcShape<128, 2>::SMEM);
+    return e;
+}
+
+// Scratch of a split product. Calls run one after another on the stream, so they share it.
+size_t split_bytes(const scalecom_ops* o, int epi, const Product& p) {
+    const Plan pl = make_plan(o, epi, p.a->planes, p.m, p.n, product_iters(p), p.batch);
+    return pl.splits > 1 ? size_t(pl.tiles) * p.batch * pl.splits * TC_BM * pl.bn * 4 : 0;
+}
+
+// P: the epilogue's fields are set by the caller
+int run_product(scalecom_ops* o, int epi, const Product& p, TcParams& P, float* partial) {
+    const Plan pl = make_plan(o, epi, p.a->planes, p.m, p.n, product_iters(p), p.batch);
+    if (pl.tiles * p.batch > 0x7FFFFFFFll / 32) return SCALECOM_ERR_INVALID_ARG;
+    const int bbox = epi == EPI_GATE ? pl.bn / 2 : pl.bn;
+    bool ok = encode(o, &P.a[0], *p.a, p.bf16, p.a_mn, TC_BM) && encode(o, &P.b[0], *p.b, p.bf16, p.b_mn, bbox);
+    if (ok && p.a2) ok = encode(o, &P.a[1], *p.a2, p.bf16, p.a_mn, TC_BM);
+    if (ok && p.b2) ok = encode(o, &P.b[1], *p.b2, p.bf16, p.b_mn, bbox);
+    if (!ok) return SCALECOM_ERR_CUDA;
+    P.pairs = p.a2 ? 2 : 1;
+    P.kblocks = int32_t(ceil_div(p.k, TC_BK));
+    P.m = int32_t(p.m);
+    P.n = int32_t(p.n);
+    P.mt = int32_t(pl.mt);
+    P.nt = int32_t(pl.nt);
+    P.tiles = int32_t(pl.tiles);
+    P.batch = p.batch;
+    P.splits = pl.splits;
+    P.a_mn = p.a_mn;
+    P.b_mn = p.b_mn;
+    P.a_batched = p.a_batched;
+    P.b_batched = p.b_batched;
+    // fp32 accumulators; both operands fp16 (0) or bf16 (1); majors; N / 8, M / 16
+    P.idesc = (1u << 4) | ((p.bf16 ? 1u : 0u) << 7) | ((p.bf16 ? 1u : 0u) << 10) | ((p.a_mn ? 1u : 0u) << 15) |
+              ((p.b_mn ? 1u : 0u) << 16) | (uint32_t(pl.bn / 8) << 17) | (uint32_t(TC_BM / 16) << 24);
+    P.status = o->ctrl;
+    P.partial = partial;
+    P.arrived = o->ctrl + 16;
+    P.amax_a = p.a->amax;
+    P.amax_b = p.b->amax;
+    cudaError_t e;
+    switch (epi) {
+        case EPI_STORE: e = tc_launch_any<EPI_STORE>(o, pl.bn, p.a->planes, P); break;
+        case EPI_GATE: e = tc_launch_any<EPI_GATE>(o, pl.bn, p.a->planes, P); break;
+        case EPI_GATE_BWD: e = tc_launch_any<EPI_GATE_BWD>(o, pl.bn, p.a->planes, P); break;
+        case EPI_GRAM: e = tc_launch_any<EPI_GRAM>(o, pl.bn, p.a->planes, P); break;
+        case EPI_POLY: e = tc_launch_any<EPI_POLY>(o, pl.bn, p.a->planes, P); break;
+        default: e = tc_launch_any<EPI_PLANES>(o, pl.bn, p.a->planes, P); break;
+    }
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return SCALECOM_ERR_CUDA;
+    }
+    return SCALECOM_OK;
+}
+
+// Operands of one call that need work before the tensor cores can read them: fp32 ones (planes), 16-bit ones off the
+// 16-byte grid. In the counting pass it only takes the scratch.
+struct Prep {
+    PrepTable t;
+    int n = 0;
+    int64_t most_rows = 0;
+    Prep(int type) { t.type = type; }
+    Operand add(Carver& c, const void* p, int64_t rows, int64_t cols, int64_t ld, uint32_t* amax) {
+        Operand a;
+        a.rows = rows;
+        a.cols = cols;
+        if (t.type != SCALECOM_F32 && tma_ready(p, ld)) {
+            a.p = p;
+            a.ld = ld;
+            return a;
+        }
+        a.ld = pad8(cols);
+        a.planes = t.type == SCALECOM_F32 ? 2 : 1;
+        a.plane = a.planes > 1 ? rows * a.ld : 0;
+        a.p = c.take<uint16_t>(a.planes * rows * a.ld);
+        a.amax = t.type == SCALECOM_F32 ? amax : nullptr;
+        t.item[n++] = {p, ld, rows, cols, const_cast<void*>(a.p), a.ld, a.plane, amax};
+        if (rows > most_rows) most_rows = rows;
+        return a;
+    }
+    int run(scalecom_ops* o, bool need_amax) {
+        if (!n) return SCALECOM_OK;
+        const int64_t cap = int64_t(o->sms) * 4;
+        const dim3 grid(unsigned(most_rows < cap ? most_rows : cap), unsigned(n));
+        if (t.type == SCALECOM_F32 && need_amax && launch(o, prep_amax_kernel, grid, PREP_THREADS, 0, t) != cudaSuccess)
+            return SCALECOM_ERR_CUDA;
+        return launch(o, prep_operand_kernel, grid, PREP_THREADS, 0, t) == cudaSuccess ? SCALECOM_OK : SCALECOM_ERR_CUDA;
+    }
+};
+
+// largest-magnitude words of a call's fp32 operands
+enum { AM_X = 0, AM_WGU, AM_WD, AM_DY, AM_H, AM_DGU, AM_WORDS };
+
+struct FfnArgs {
+    int type, act;
+    int64_t tokens, width, hidden;
+    const void *x, *wg, *wu, *wd;
+    int64_t ldx;
+};
+
+int ffn_forward(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* saved) {
+    const bool f32 = A.type == SCALECOM_F32, bf16 = A.type == SCALECOM_BF16;
+    const int64_t T = A.tokens, d = A.width, f = A.hidden, fp = pad8(f);
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c{pass ? static_cast<char*>(o->ws) : nullptr};
+        uint32_t* am = c.take<uint32_t>(AM_WORDS);
+        Prep prep(A.type), prep_h(A.type);
+        const Operand x = prep.add(c, A.x, T, d, A.ldx, am + AM_X);
+        const Operand wg = prep.add(c, A.wg, f, d, d, am + AM_WGU), wu = prep.add(c, A.wu, f, d, d, am + AM_WGU);
+        const Operand wd = prep.add(c, A.wd, d, f, f, am + AM_WD);
+        void* h = f32 ? static_cast<void*>(c.take<float>(T * fp)) : static_cast<void*>(c.take<uint16_t>(T * fp));
+        Operand ho;
+        if (f32) {
+            ho = prep_h.add(c, h, T, f, fp, am + AM_H);
+        } else {
+            ho.p = h;
+            ho.rows = T;
+            ho.cols = f;
+            ho.ld = fp;
+        }
+        Product up, down;
+        up.a = &x; up.b = &wg; up.b2 = &wu; up.bf16 = bf16;
+        up.m = T; up.n = f; up.k = d;
+        down.a = &ho; down.b = &wd; down.bf16 = bf16;
+        down.m = T; down.n = d; down.k = f;
+        const size_t s1 = split_bytes(o, EPI_GATE, up), s2 = split_bytes(o, EPI_STORE, down);
+        float* partial = reinterpret_cast<float*>(c.take<char>(int64_t(s1 > s2 ? s1 : s2)));
+        if (!pass) {
+            const int rc = ensure_ws(o, c.used);
+            if (rc != SCALECOM_OK) return rc;
+            continue;
+        }
+        if (f32 && cudaMemsetAsync(am, 0, AM_WORDS * 4, o->stream) != cudaSuccess) return SCALECOM_ERR_CUDA;
+        int rc = prep.run(o, true);
+        if (rc != SCALECOM_OK) return rc;
+        TcParams P;
+        std::memset(&P, 0, sizeof P);
+        P.type = A.type;
+        P.act = A.act;
+        P.alpha = 1.0f;
+        P.out = h;
+        P.ldo = fp;
+        P.out2 = saved;
+        P.amax_o = f32 ? am + AM_H : nullptr;
+        rc = run_product(o, EPI_GATE, up, P, partial);
+        if (rc == SCALECOM_OK) rc = prep_h.run(o, false);
+        if (rc != SCALECOM_OK) return rc;
+        std::memset(&P, 0, sizeof P);
+        P.type = A.type;
+        P.alpha = 1.0f;
+        P.out = y;
+        P.ldo = ldy;
+        return run_product(o, EPI_STORE, down, P, partial);
+    }
+    return SCALECOM_ERR_INTERNAL;
+}
+
+int ffn_backward(scalecom_ops* o, const FfnArgs& A, int wgrad_type, const void* dy, int64_t lddy, const void* saved, void* dx,
+                 int64_t lddx, void* dwg, void* dwu, void* dwd) {
+    const bool f32 = A.type == SCALECOM_F32, bf16 = A.type == SCALECOM_BF16;
+    const int64_t T = A.tokens, d = A.width, f = A.hidden, fp = pad8(f);
+    const int64_t e = type_size(A.type);
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c{pass ? static_cast<char*>(o->ws) : nullptr};
+        uint32_t* am = c.take<uint32_t>(AM_WORDS);
+        Prep prep(A.type), prep_mid(A.type);
+        const Operand dyo = prep.add(c, dy, T, d, lddy, am + AM_DY);
+        const Operand wd = prep.add(c, A.wd, d, f, f, am + AM_WD);
+        Operand x, wg, wu;
+        if (dwg || dwu) x = prep.add(c, A.x, T, d, A.ldx, am + AM_X);
+        if (dx) {
+            wg = prep.add(c, A.wg, f, d, d, am + AM_WGU);
+            wu = prep.add(c, A.wu, f, d, d, am + AM_WGU);
+        }
+        // dg, du and h: [3][tokens][fp] in the call's type
+        char* mid = c.take<char>(3 * T * fp * e);
+        Operand dg, du, h;
+        if (f32) {
+            // dg and du share a scale: their products are summed in one accumulator
+            dg = prep_mid.add(c, mid, T, f, fp, am + AM_DGU);
+            du = prep_mid.add(c, mid ? mid + T * fp * e : nullptr, T, f, fp, am + AM_DGU);
+            h = prep_mid.add(c, mid ? mid + 2 * T * fp * e : nullptr, T, f, fp, am + AM_H);
+        } else {
+            dg.rows = T; dg.cols = f; dg.ld = fp;
+            du = dg; h = dg;
+            dg.p = mid;
+            du.p = mid ? mid + T * fp * e : nullptr;
+            h.p = mid ? mid + 2 * T * fp * e : nullptr;
+        }
+        Product pdh, pdx, pwg, pwu, pwd;
+        pdh.a = &dyo; pdh.b = &wd; pdh.b_mn = true; pdh.bf16 = bf16;
+        pdh.m = T; pdh.n = f; pdh.k = d;
+        pdx.a = &dg; pdx.a2 = &du; pdx.b = &wg; pdx.b2 = &wu; pdx.b_mn = true; pdx.bf16 = bf16;
+        pdx.m = T; pdx.n = d; pdx.k = f;
+        pwg.a = &dg; pwg.b = &x; pwg.a_mn = pwg.b_mn = true; pwg.bf16 = bf16;
+        pwg.m = f; pwg.n = d; pwg.k = T;
+        pwu = pwg;
+        pwu.a = &du;
+        pwd.a = &dyo; pwd.b = &h; pwd.a_mn = pwd.b_mn = true; pwd.bf16 = bf16;
+        pwd.m = d; pwd.n = f; pwd.k = T;
+        size_t most = split_bytes(o, EPI_GATE_BWD, pdh);
+        auto more = [&](size_t s) { if (s > most) most = s; };
+        if (dx) more(split_bytes(o, EPI_STORE, pdx));
+        if (dwg || dwu) more(split_bytes(o, EPI_STORE, pwg));
+        if (dwd) more(split_bytes(o, EPI_STORE, pwd));
+        float* partial = reinterpret_cast<float*>(c.take<char>(int64_t(most)));
+        if (!pass) {
+            const int rc = ensure_ws(o, c.used);
+            if (rc != SCALECOM_OK) return rc;
+            continue;
+        }
+        if (f32 && cudaMemsetAsync(am, 0, AM_WORDS * 4, o->stream) != cudaSuccess) return SCALECOM_ERR_CUDA;
+        int rc = prep.run(o, true);
+        if (rc != SCALECOM_OK) return rc;
+        TcParams P;
+        std::memset(&P, 0, sizeof P);
+        P.type = A.type;
+        P.act = A.act;
+        P.alpha = 1.0f;
+        P.in1 = saved;
+        P.in2 = static_cast<const char*>(saved) + T * f * e;
+        P.ldi = f;
+        P.out = mid;
+        P.out2 = mid + T * fp * e;
+        P.out3 = mid + 2 * T * fp * e;
+        P.ldo = fp;
+        P.amax_o = f32 ? am + AM_DGU : nullptr;
+        P.amax_o2 = f32 ? am + AM_H : nullptr;
+        rc = run_product(o, EPI_GATE_BWD, pdh, P, partial);
+        if (rc == SCALECOM_OK) rc = prep_mid.run(o, false);
+        if (rc != SCALECOM_OK) return rc;
+        auto store = [&](const Product& p, void* out, int type, int64_t ld) {
+            TcParams Q;
+            std::memset(&Q, 0, sizeof Q);
+            Q.type = type;
+            Q.alpha = 1.0f;
+            Q.out = out;
+            Q.ldo = ld;
+            return run_product(o, EPI_STORE, p, Q, partial);
+        };
+        if (dx) rc = store(pdx, dx, A.type, lddx);
+        if (rc == SCALECOM_OK && dwg) rc = store(pwg, dwg, wgrad_type, d);
+        if (rc == SCALECOM_OK && dwu) rc = store(pwu, dwu, wgrad_type, d);
+        if (rc == SCALECOM_OK && dwd) rc = store(pwd, dwd, wgrad_type, f);
+        return rc;
+    }
+    return SCALECOM_ERR_INTERNAL;
+}
+
+// ---- Newton-Schulz -----------------------------------------------------------------------------------------------
+// X, A and bA + cAA + aI are held as 2^10 times themselves in fp16 planes: entries up to 63 fit, and the smallest
+// entries that matter (1 / sqrt(rows * cols) of a normalised matrix) stay far above fp16's subnormals.
+constexpr double NS_SCALE = 1024.0;
+
+struct NsArgs {
+    int64_t batch, rows, cols;
+    int in_type, out_type;
+    const void* in;
+    void* out;
+    int64_t ld_in, in_stride, ld_out, out_stride;
+    int steps, ncoef;
+    const float* co;
+    float eps, scale;
+};
+
+int orthogonalise(scalecom_ops* o, const NsArgs& A) {
+    const int planes = A.out_type == SCALECOM_F32 ? 2 : 1;
+    const bool tall = A.rows > A.cols;
+    const int64_t r = tall ? A.cols : A.rows, big = tall ? A.rows : A.cols;
+    const int64_t ldx = pad8(A.cols), lda = pad8(r), B = A.batch;
+    int64_t nparts = ceil_div(A.rows * A.cols, 1 << 14);
+    if (nparts > ceil_div(int64_t(o->sms) * 4, B)) nparts = ceil_div(int64_t(o->sms) * 4, B);
+    if (nparts > A.rows) nparts = A.rows;
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c{pass ? static_cast<char*>(o->ws) : nullptr};
+        double* part = c.take<double>(B * nparts);
+        Operand x[2], g, q;
+        if (A.steps) {
+            for (int i = 0; i < (A.steps > 1 ? 2 : 1); ++i) {
+                x[i].rows = A.rows; x[i].cols = A.cols; x[i].ld = ldx;
+                x[i].planes = planes;
+                x[i].plane = planes > 1 ? A.rows * ldx : 0;
+                x[i].batch = int(B);
+                x[i].stride = planes * A.rows * ldx;
+                x[i].p = c.take<__half>(B * x[i].stride);
+            }
+            g.rows = g.cols = r;
+            g.ld = lda;
+            g.planes = planes;
+            g.plane = planes > 1 ? r * lda : 0;
+            g.batch = int(B);
+            g.stride = planes * r * lda;
+            q = g;
+            g.p = c.take<__half>(B * g.stride);
+            q.p = c.take<__half>(B * q.stride);
+        }
+        Product gram, poly, apply;
+        gram.m = gram.n = r; gram.k = big;
+        gram.a_mn = gram.b_mn = tall;
+        gram.a = gram.b = &x[0];
+        gram.a_batched = gram.b_batched = true;
+        gram.batch = int(B);
+        poly = gram;
+        poly.a_mn = poly.b_mn = false;
+        poly.k = r;
+        poly.a = poly.b = &g;
+        apply = gram;
+        apply.m = A.rows; apply.n = A.cols; apply.k = r;
+        apply.a_mn = false;
+        apply.b_mn = !tall;
+        apply.a = tall ? &x[0] : &q;
+        apply.b = tall ? &q : &x[0];
+        size_t most = 0;
+        if (A.steps) {
+            const size_t s[3] = {split_bytes(o, EPI_GRAM, gram), split_bytes(o, EPI_POLY, poly), split_bytes(o, EPI_PLANES, apply)};
+            for (size_t v : s) if (v > most) most = v;
+        }
+        float* partial = reinterpret_cast<float*>(c.take<char>(int64_t(most)));
+        if (!pass) {
+            const int rc = ensure_ws(o, c.used);
+            if (rc != SCALECOM_OK) return rc;
+            continue;
+        }
+        NormParams N;
+        std::memset(&N, 0, sizeof N);
+        N.in = A.in; N.ld = A.ld_in; N.stride = A.in_stride;
+        N.rows = A.rows; N.cols = A.cols; N.in_type = A.in_type;
+        N.partial = part; N.nparts = int32_t(nparts);
+        N.eps = A.eps;
+        if (A.steps) {
+            N.factor = NS_SCALE;
+            N.planes = const_cast<__half*>(static_cast<const __half*>(x[0].p));
+            N.planes_ld = ldx; N.planes_lo = x[0].plane; N.planes_stride = x[0].stride;
+        } else {
+            N.factor = A.scale;
+            N.out = A.out; N.out_type = A.out_type; N.ld_out = A.ld_out; N.out_stride = A.out_stride;
+        }
+        const dim3 grid{unsigned(nparts), unsigned(B)};
+        if (launch(o, norm_partial_kernel, grid, PREP_THREADS, 0, N) != cudaSuccess ||
+            launch(o, norm_apply_kernel, grid, PREP_THREADS, 0, N) != cudaSuccess) {
+            cudaGetLastError();
+            return SCALECOM_ERR_CUDA;
+        }
+        for (int s = 0; s < A.steps; ++s) {
+            const float* co = A.co + (A.ncoef > 1 ? 3 * s : 0);
+            const Operand *now = &x[s & 1], *next = &x[(s & 1) ^ 1];
+            TcParams P;
+            std::memset(&P, 0, sizeof P);
+            gram.a = gram.b = now;
+            P.alpha = float(1.0 / NS_SCALE);
+            P.planes_out = const_cast<__half*>(static_cast<const __half*>(g.p));
+            P.plane_out = g.plane; P.ostride = g.stride; P.ldo = lda;
+            int rc = run_product(o, EPI_GRAM, gram, P, partial);
+            if (rc != SCALECOM_OK) return rc;
+            std::memset(&P, 0, sizeof P);
+            P.poly_a = float(co[0] * NS_SCALE); P.poly_b = co[1]; P.poly_c = float(co[2] / NS_SCALE);
+            P.planes_in = static_cast<const __half*>(g.p);
+            P.plane_in = g.plane;
+            P.planes_out = const_cast<__half*>(static_cast<const __half*>(q.p));
+            P.plane_out = q.plane; P.ostride = q.stride; P.ldo = lda;
+            rc = run_product(o, EPI_POLY, poly, P, partial);
+            if (rc != SCALECOM_OK) return rc;
+            std::memset(&P, 0, sizeof P);
+            (tall ? apply.a : apply.b) = now;
+            if (s + 1 < A.steps) {
+                P.alpha = float(1.0 / NS_SCALE);
+                P.planes_out = const_cast<__half*>(static_cast<const __half*>(next->p));
+                P.plane_out = next->plane; P.ostride = next->stride; P.ldo = ldx;
+                rc = run_product(o, EPI_PLANES, apply, P, partial);
+            } else {
+                P.alpha = float(double(A.scale) / (NS_SCALE * NS_SCALE));
+                P.type = A.out_type;
+                P.out = A.out; P.ldo = A.ld_out; P.ostride = A.out_stride;
+                rc = run_product(o, EPI_STORE, apply, P, partial);
+            }
+            if (rc != SCALECOM_OK) return rc;
+        }
+        return SCALECOM_OK;
+    }
+    return SCALECOM_ERR_INTERNAL;
+}
+
+bool same(const void* a, const void* b) { return a && a == b; }
+
+}  // namespace
+
+extern "C" {
+
+int scalecom_ops_create(scalecom_ops** out) {
+    if (!out) return SCALECOM_ERR_NULL_PTR;
+    *out = nullptr;
+    scalecom_ops* o = new (std::nothrow) scalecom_ops;
+    if (!o) return SCALECOM_ERR_ALLOC;
+    int major = 0, minor = 0;
+    cudaError_t e = cudaGetDevice(&o->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&o->sms, cudaDevAttrMultiProcessorCount, o->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, o->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, o->device);
+    if (e == cudaSuccess && (major != 10 || minor != 0)) e = cudaErrorNoKernelImageForDevice;
+    if (e == cudaSuccess) {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+        if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !fn)) e = cudaErrorSymbolNotFound;
+        o->encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled>(fn);
+    }
+    if (e == cudaSuccess) e = tc_attributes<EPI_STORE>();
+    if (e == cudaSuccess) e = tc_attributes<EPI_GATE>();
+    if (e == cudaSuccess) e = tc_attributes<EPI_GATE_BWD>();
+    if (e == cudaSuccess) e = tc_attributes<EPI_GRAM>();
+    if (e == cudaSuccess) e = tc_attributes<EPI_POLY>();
+    if (e == cudaSuccess) e = tc_attributes<EPI_PLANES>();
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        delete o;
+        return SCALECOM_ERR_CUDA;
+    }
+    if (cudaMalloc(reinterpret_cast<void**>(&o->ctrl), CTRL_WORDS * 4) != cudaSuccess) {
+        cudaGetLastError();
+        delete o;
+        return SCALECOM_ERR_ALLOC;
+    }
+    if (cudaMemset(o->ctrl, 0, CTRL_WORDS * 4) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
+        cudaGetLastError();
+        scalecom_ops_destroy(o);
+        return SCALECOM_ERR_CUDA;
+    }
+    *out = o;
+    return SCALECOM_OK;
+}
+
+void scalecom_ops_destroy(scalecom_ops* o) {
+    if (!o) return;
+    DeviceGuard guard(o->device);
+    cudaStreamSynchronize(o->stream);
+    cudaFree(o->ws);
+    cudaFree(o->ctrl);
+    cudaGetLastError();
+    delete o;
+}
+
+int scalecom_ops_set_stream(scalecom_ops* o, void* cuda_stream) {
+    if (!o) return SCALECOM_ERR_NULL_PTR;
+    DeviceGuard guard(o->device);
+    if (!guard.ok) return SCALECOM_ERR_CUDA;
+    if (cudaStreamSynchronize(o->stream) != cudaSuccess) return SCALECOM_ERR_CUDA;   // scratch is shared between calls
+    o->stream = static_cast<cudaStream_t>(cuda_stream);
+    return SCALECOM_OK;
+}
+
+int scalecom_ops_reserve(scalecom_ops* o, int64_t bytes) {
+    if (!o) return SCALECOM_ERR_NULL_PTR;
+    if (bytes < 0) return SCALECOM_ERR_INVALID_ARG;
+    DeviceGuard guard(o->device);
+    if (!guard.ok) return SCALECOM_ERR_CUDA;
+    return ensure_ws(o, size_t(bytes));
+}
+
+int scalecom_ops_workspace(const scalecom_ops* o, int64_t* bytes) {
+    if (!o || !bytes) return SCALECOM_ERR_NULL_PTR;
+    *bytes = int64_t(o->ws_bytes);
+    return SCALECOM_OK;
+}
+
+int scalecom_ops_status(scalecom_ops* o) {
+    if (!o) return SCALECOM_ERR_NULL_PTR;
+    DeviceGuard guard(o->device);
+    uint32_t st = 0;
+    if (!guard.ok || cudaStreamSynchronize(o->stream) != cudaSuccess ||
+        cudaMemcpy(&st, o->ctrl, 4, cudaMemcpyDeviceToHost) != cudaSuccess) {
+        o->poisoned = true;
+        return SCALECOM_ERR_CUDA;
+    }
+    if (st == DEV_OK) return SCALECOM_OK;
+    o->poisoned = true;
+    return st == DEV_TIMEOUT ? SCALECOM_ERR_TIMEOUT : SCALECOM_ERR_INTERNAL;
+}
+
+int scalecom_ops_reset(scalecom_ops* o) {
+    if (!o) return SCALECOM_ERR_NULL_PTR;
+    DeviceGuard guard(o->device);
+    if (!guard.ok || cudaStreamSynchronize(o->stream) != cudaSuccess ||
+        cudaMemset(o->ctrl, 0, CTRL_WORDS * 4) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess)
+        return SCALECOM_ERR_CUDA;
+    o->poisoned = false;
+    return SCALECOM_OK;
+}
+
+int scalecom_layer_norm(scalecom_ops* o, int32_t dtype, int64_t rows, int64_t width, const void* x, int64_t ldx, const float* gamma,
+                        const float* beta, float eps, void* y, int64_t ldy, float* mean, float* rstd) {
+    int rc = enter(o);
+    if (rc != SCALECOM_OK) return rc;
+    if (!type_ok(dtype) || !dim_ok(rows, 0) || !dim_ok(width, 1) || ldx < width || ldy < width || !(eps >= 0.0f) || !std::isfinite(eps))
+        return SCALECOM_ERR_INVALID_ARG;
+    if (rows == 0) return SCALECOM_OK;
+    if (!x || !y) return SCALECOM_ERR_NULL_PTR;
+    if ((x == y && ldx != ldy) || same(y, gamma) || same(y, beta) || same(y, mean) || same(y, rstd) || same(mean, rstd) ||
+        same(x, mean) || same(x, rstd))
+        return SCALECOM_ERR_ALIAS;
+    DeviceGuard guard(o->device);
+    if (!guard.ok) return SCALECOM_ERR_CUDA;
+    LnParams P;
+    std::memset(&P, 0, sizeof P);
+    P.x = x; P.y = y; P.gamma = gamma; P.beta = beta; P.mean = mean; P.rstd = rstd;
+    P.ldx = ldx; P.ldy = ldy; P.rows = rows; P.width = int32_t(width); P.eps = eps;
+    cudaError_t e = dtype == SCALECOM_F32 ? ln_forward_t<float>(o, P)
+                  : dtype == SCALECOM_F16 ? ln_forward_t<__half>(o, P) : ln_forward_t<__nv_bfloat16>(o, P);
+    if (e != cudaSuccess) { cudaGetLastError(); return SCALECOM_ERR_CUDA; }
+    return SCALECOM_OK;
+}
+
+int scalecom_layer_norm_backward(scalecom_ops* o, int32_t dtype, int64_t rows, int64_t width, const void* dy, int64_t lddy, const void* x,
+                                 int64_t ldx, const float* gamma, const float* mean, const float* rstd, void* dx, int64_t lddx,
+                                 float* dgamma, float* dbeta) {
+    int rc = enter(o);
+    if (rc != SCALECOM_OK) return rc;
+    if (!type_ok(dtype) || !dim_ok(rows, 0) || !dim_ok(width, 1) || ldx < width || lddy < width || (dx && lddx < width))
+        return SCALECOM_ERR_INVALID_ARG;
+    DeviceGuard guard(o->device);
+    if (!guard.ok) return SCALECOM_ERR_CUDA;
+    if (same(dgamma, dbeta)) return SCALECOM_ERR_ALIAS;
+    if (rows == 0) {
+        if ((dgamma && cudaMemsetAsync(dgamma, 0, size_t(width) * 4, o->stream) != cudaSuccess) ||
+            (dbeta && cudaMemsetAsync(dbeta, 0, size_t(width) * 4, o->stream) != cudaSuccess))
+            return SCALECOM_ERR_CUDA;
+        return SCALECOM_OK;
+    }
+    if (!dy || !x || !mean || !rstd) return SCALECOM_ERR_NULL_PTR;
+    if (same(dx, x) || (same(dx, dy) && lddx != lddy) || same(dx, gamma) || same(dx, mean) || same(dx, rstd) || same(dx, dgamma) ||
+        same(dx, dbeta) || same(dgamma, dy) || same(dbeta, dy) || same(dgamma, x) || same(dbeta, x) || same(dgamma, gamma) ||
+        same(dbeta, gamma) || same(dgamma, mean) || same(dbeta, mean) || same(dgamma, rstd) || same(dbeta, rstd))
+        return SCALECOM_ERR_ALIAS;
+    if (!dx && !dgamma && !dbeta) return SCALECOM_OK;
+    const bool dw = dgamma || dbeta;
+    if (dw) {
+        rc = ensure_ws(o, size_t(o->sms) * 2 * 2 * size_t(width) * 4);
+        if (rc != SCALECOM_OK) return rc;
+    }
+    LnParams P;
+    std::memset(&P, 0, sizeof P);
+    P.x = x; P.dy = dy; P.dx = dx; P.gamma = gamma; P.mean_in = mean; P.rstd_in = rstd;
+    P.dgamma = dgamma; P.dbeta = dbeta; P.partial = static_cast<float*>(o->ws);
+    P.ldx = ldx; P.lddy = lddy; P.lddx = lddx; P.rows = rows; P.width = int32_t(width);
+    cudaError_t e = dtype == SCALECOM_F32 ? ln_backward_t<float>(o, P)
+                  : dtype == SCALECOM_F16 ? ln_backward_t<__half>(o, P) : ln_backward_t<__nv_bfloat16>(o, P);
+    if (e == cudaSuccess && dw)
+        e = launch(o, layer_norm_reduce_kernel, dim3(unsigned(ceil_div(2 * width, 32))), LN_THREADS, 0, P);
+    if (e != cudaSuccess) { cudaGetLastError(); return SCALECOM_ERR_CUDA; }
+    return SCALECOM_OK;
+}
+
+int scalecom_gated_ffn(scalecom_ops* o, int32_t dtype, int32_t act, int64_t tokens, int64_t width, int64_t hidden, const void* x, int64_t ldx,
+                       const void* w_gate, const void* w_up, const void* w_down, void* y, int64_t ldy, void* saved) {
+    int rc = enter(o);
+    if (rc != SCALECOM_OK) return rc;
+    if (!type_ok(dtype) || act < SCALECOM_ACT_SILU || act > SCALECOM_ACT_RELU || !dim_ok(tokens, 0) || !dim_ok(width, 1) ||
+        !dim_ok(hidden, 1) || ldx < width || ldy < width)
+        return SCALECOM_ERR_INVALID_ARG;
+    if (tokens == 0) return SCALECOM_OK;
+    if (!x || !w_gate || !w_up || !w_down || !y) return SCALECOM_ERR_NULL_PTR;
+    for (const void* p : {x, w_gate, w_up, w_down, static_cast<const void*>(y)})
+        if (same(saved, p) || (p != y && same(y, p))) return SCALECOM_ERR_ALIAS;
+    DeviceGuard guard(o->device);
+    if (!guard.ok) return SCALECOM_ERR_CUDA;
+    const FfnArgs A = {dtype, act, tokens, width, hidden, x, w_gate, w_up, w_down, ldx};
+    rc = ffn_forward(o, A, y, ldy, saved);
+    if (rc == SCALECOM_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+int scalecom_gated_ffn_backward(scalecom_ops* o, int32_t dtype, int32_t wgrad_type, int32_t act, int64_t tokens, int64_t width, int64_t hidden,
+                                const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_gate, const void* w_up,
+                                const void* w_down, const void* saved, void* dx, int64_t lddx, void* dw_gate, void* dw_up, void* dw_down) {
+    int rc = enter(o);
+    if (rc != SCALECOM_OK) return rc;
+    if (!type_ok(dtype) || (wgrad_type != dtype && wgrad_type != SCALECOM_F32) || act < SCALECOM_ACT_SILU || act > SCALECOM_ACT_RELU ||
+        !dim_ok(tokens, 0) || !dim_ok(width, 1) || !dim_ok(hidden, 1) || ldx < width || lddy < width || (dx && lddx < width))
+        return SCALECOM_ERR_INVALID_ARG;
+    DeviceGuard guard(o->device);
+    if (!guard.ok) return SCALECOM_ERR_CUDA;
+    void* outs[4] = {dx, dw_gate, dw_up, dw_down};
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < i; ++j)
+            if (same(outs[i], outs[j])) return SCALECOM_ERR_ALIAS;
+    if (tokens == 0) {
+        for (int i = 1; i < 4; ++i)
+            if (outs[i] && cudaMemsetAsync(outs[i], 0, size_t(width) * hidden * type_size(wgrad_type), o->stream) != cudaSuccess)
+                return SCALECOM_ERR_CUDA;
+        return SCALECOM_OK;
+    }
+    if (!dy || !x || !w_gate || !w_up || !w_down || !saved) return SCALECOM_ERR_NULL_PTR;
+    for (const void* p : {dy, x, w_gate, w_up, w_down, saved})
+        for (void* q : outs)
+            if (same(q, p)) return SCALECOM_ERR_ALIAS;
+    if (!dx && !dw_gate && !dw_up && !dw_down) return SCALECOM_OK;
+    const FfnArgs A = {dtype, act, tokens, width, hidden, x, w_gate, w_up, w_down, ldx};
+    rc = ffn_backward(o, A, wgrad_type, dy, lddy, saved, dx, lddx, dw_gate, dw_up, dw_down);
+    if (rc == SCALECOM_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+int scalecom_orthogonalise(scalecom_ops* o, int64_t batch, int64_t rows, int64_t cols, int32_t in_type, const void* in, int64_t ld_in,
+                           int64_t in_stride, int32_t out_type, void* out, int64_t ld_out, int64_t out_stride, int32_t steps,
+                           const float* coefficients, int32_t ncoef, float eps, float scale) {
+    int rc = enter(o);
+    if (rc != SCALECOM_OK) return rc;
+    if (!type_ok(in_type) || !type_ok(out_type) || !dim_ok(rows, 1) || !dim_ok(cols, 1) || batch < 0 || batch > 65535 || ld_in < cols ||
+        ld_out < cols || steps < 0 || steps > 64 || !(eps >= 0.0f) || !std::isfinite(eps) || !std::isfinite(scale))
+        return SCALECOM_ERR_INVALID_ARG;
+    if (batch > 1 && (in_stride < (rows - 1) * ld_in + cols || out_stride < (rows - 1) * ld_out + cols)) return SCALECOM_ERR_INVALID_ARG;
+    if (steps > 0) {
+        if (!coefficients) return SCALECOM_ERR_NULL_PTR;
+        if (ncoef != 1 && ncoef != steps) return SCALECOM_ERR_INVALID_ARG;
+        for (int i = 0; i < 3 * ncoef; ++i)
+            if (!(std::fabs(coefficients[i]) <= 63.0f)) return SCALECOM_ERR_INVALID_ARG;
+    }
+    if (batch == 0) return SCALECOM_OK;
+    if (!in || !out) return SCALECOM_ERR_NULL_PTR;
+    if (in == out && (in_type != out_type || ld_in != ld_out || (batch > 1 && in_stride != out_stride))) return SCALECOM_ERR_ALIAS;
+    DeviceGuard guard(o->device);
+    if (!guard.ok) return SCALECOM_ERR_CUDA;
+    const NsArgs A = {batch, rows, cols, in_type, out_type, in, out, ld_in, in_stride, ld_out, out_stride, steps, ncoef, coefficients, eps, scale};
+    rc = orthogonalise(o, A);
+    if (rc == SCALECOM_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+}  // extern "C"

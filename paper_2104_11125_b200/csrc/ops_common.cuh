@@ -1,0 +1,124 @@
+// Shared helpers of the learner-side operators: element types, vector access, waits.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/scalecom_operators.h"
+#include "common.cuh"
+
+namespace sc {
+
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+    static constexpr int id = SCALECOM_F32;
+    static __device__ __forceinline__ float up(float v) { return v; }
+    static __device__ __forceinline__ float down(float v) { return v; }
+};
+template <> struct Elem<__half> {
+    static constexpr int id = SCALECOM_F16;
+    static __device__ __forceinline__ float up(__half v) { return __half2float(v); }
+    static __device__ __forceinline__ __half down(float v) { return __float2half_rn(v); }
+};
+template <> struct Elem<__nv_bfloat16> {
+    static constexpr int id = SCALECOM_BF16;
+    static __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
+    static __device__ __forceinline__ __nv_bfloat16 down(float v) { return __float2bfloat16_rn(v); }
+};
+
+// N elements of T as one object that a single load or store moves (N * sizeof(T) <= 16)
+template <typename T, int N> struct alignas(N * sizeof(T)) Pack { T e[N]; };
+
+template <typename T, int N>
+__device__ __forceinline__ void load_up(const T* p, float (&v)[N]) {
+    const Pack<T, N> t = *reinterpret_cast<const Pack<T, N>*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = Elem<T>::up(t.e[i]);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_down(T* p, const float (&v)[N]) {
+    Pack<T, N> t;
+#pragma unroll
+    for (int i = 0; i < N; ++i) t.e[i] = Elem<T>::down(v[i]);
+    *reinterpret_cast<Pack<T, N>*>(p) = t;
+}
+
+// 32 consecutive elements of one row: 16-byte accesses where the address and the row's end allow it
+template <typename T>
+__device__ __forceinline__ void store_row32(T* p, const float* v, int ncols) {
+    constexpr int N = 16 / sizeof(T);
+    if (ncols >= 32 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+#pragma unroll
+        for (int i = 0; i < 32; i += N) {
+            float t[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) t[j] = v[i + j];
+            store_down<T, N>(p + i, t);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < ncols) p[i] = Elem<T>::down(v[i]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load_row32(const T* p, float* v, int ncols) {
+    constexpr int N = 16 / sizeof(T);
+    if (ncols >= 32 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+#pragma unroll
+        for (int i = 0; i < 32; i += N) {
+            float t[N];
+            load_up<T, N>(p + i, t);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[i + j] = t[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = i < ncols ? Elem<T>::up(p[i]) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ float warp_sum_f(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max_f(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
+    return v;
+}
+
+// ---- chains of launches ------------------------------------------------------------------------------
+// Every kernel of an operator is launched with programmatic stream serialisation: its blocks may start while the
+// kernel before it drains, and each waits here, before its first access to global memory, until that kernel has
+// completed and its writes are visible.
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chain_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// ---- power-of-two scales of fp32 operands --------------------------------------------------------------
+// A tensor's largest finite magnitude (bits in a device word) gives the scale 2^(14 - e), e its exponent: the
+// scaled values are below 2^15, inside fp16's range with room for rounding up.
+__device__ __forceinline__ float plane_scale(uint32_t amax_bits) {
+    int e = int(amax_bits >> 23) - 127;              // -127 for zero and denormals
+    int s = 14 - e;
+    if (amax_bits == 0u) s = 0;
+    if (s > 126) s = 126;                            // both 2^s and 2^-s are normal numbers
+    return __uint_as_float(uint32_t(s + 127) << 23);
+}
+__device__ __forceinline__ float plane_unscale(uint32_t amax_bits) { return 1.0f / plane_scale(amax_bits); }
+
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+    const uint32_t b = mag_key(v);
+    return b < 0x7F800000u ? b : 0u;
+}
+
+// v as two fp16 values hi + lo (22 mantissa bits); an infinity or NaN stays in hi alone
+__device__ __forceinline__ void split_planes(float v, __half& hi, __half& lo) {
+    hi = __float2half_rn(v);
+    const float r = v - __half2float(hi);
+    lo = __float2half_rn((mag_key(r) < 0x7F800000u) ? r : 0.0f);
+}
+
+}  // namespace sc
