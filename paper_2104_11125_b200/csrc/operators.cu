@@ -812,8 +812,9 @@ int scalecom_gated_ffn(scalecom_ops* o, int32_t dtype, int32_t act, int64_t toke
         return SCALECOM_ERR_INVALID_ARG;
     if (tokens == 0) return SCALECOM_OK;
     if (!x || !w_gate || !w_up || !w_down || !y) return SCALECOM_ERR_NULL_PTR;
-    for (const void* p : {x, w_gate, w_up, w_down, static_cast<const void*>(y)})
-        if (same(saved, p) || (p != y && same(y, p))) return SCALECOM_ERR_ALIAS;
+    for (const void* p : {x, w_gate, w_up, w_down})
+        if (same(saved, p) || same(y, p)) return SCALECOM_ERR_ALIAS;
+    if (same(saved, y)) return SCALECOM_ERR_ALIAS;
     DeviceGuard guard(o->device);
     if (!guard.ok) return SCALECOM_ERR_CUDA;
     const FfnArgs A = {dtype, act, tokens, width, hidden, x, w_gate, w_up, w_down, ldx};
