@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <utility>
 
 #include "layer_norm.cuh"
 #include "operand_prep.cuh"
@@ -77,18 +78,26 @@ struct Carver {
 };
 
 template <typename... A, typename... B>
-cudaError_t launch(scalecom_ops* o, void (*kernel)(A...), dim3 grid, int threads, size_t smem, B&&... args) {
+cudaError_t launch_cluster(scalecom_ops* o, int cluster, void (*kernel)(A...), dim3 grid, int threads, size_t smem, B&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = o->stream;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = unsigned(cluster);
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<A>(args)...);
+}
+template <typename... A, typename... B>
+cudaError_t launch(scalecom_ops* o, void (*kernel)(A...), dim3 grid, int threads, size_t smem, B&&... args) {
+    return launch_cluster(o, 1, kernel, grid, threads, smem, std::forward<B>(args)...);
 }
 
 int enter(scalecom_ops* o) { return !o ? SCALECOM_ERR_NULL_PTR : o->poisoned ? SCALECOM_ERR_BAD_STATE : SCALECOM_OK; }
@@ -190,6 +199,52 @@ bool encode(scalecom_ops* o, CUtensorMap* map, const Operand& a, bool bf16, bool
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// A matrix that an epilogue reads or writes in blocks of 32 x 32: [batch][planes][rows][ld] of `type`. Through a tensor map
+// where its rows start on the 16-byte grid.
+struct Surface {
+    const void* p = nullptr;
+    int type = SCALECOM_F16;
+    int64_t rows = 0, cols = 0, ld = 0;
+    int planes = 1;
+    int64_t plane = 0;
+    int batch = 1;
+    int64_t stride = 0;
+};
+Surface surface(const Operand& a) {
+    Surface r;
+    r.p = a.p; r.rows = a.rows; r.cols = a.cols; r.ld = a.ld; r.planes = a.planes; r.plane = a.plane; r.batch = a.batch; r.stride = a.stride;
+    return r;
+}
+bool block_map(scalecom_ops* o, CUtensorMap* map, const Surface& a, int32_t* tma) {
+    const int64_t e = type_size(a.type), grid = 16 / e;
+    *tma = (reinterpret_cast<uintptr_t>(a.p) & 15u) == 0 && a.ld % grid == 0 && (a.planes == 1 || a.plane % grid == 0) &&
+           (a.batch == 1 || a.stride % grid == 0);
+    if (!*tma) return true;
+    const int64_t lead = a.rows * a.ld * e;
+    cuuint64_t dims[4] = {cuuint64_t(a.cols), cuuint64_t(a.rows), cuuint64_t(a.planes), cuuint64_t(a.batch)};
+    cuuint64_t strides[3] = {cuuint64_t(a.ld * e), cuuint64_t(a.planes > 1 ? a.plane * e : lead), cuuint64_t(a.batch > 1 ? a.stride * e : lead)};
+    cuuint32_t box[4] = {32, 32, 1, 1}, el[4] = {1, 1, 1, 1};
+    const CUtensorMapDataType type = a.type == SCALECOM_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : a.type == SCALECOM_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    return o->encode(map, type, 4, const_cast<void*>(a.p), dims, strides, box, el, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     e == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool set_out(scalecom_ops* o, TcParams& P, int k, const Surface& a) {
+    P.out[k].base = static_cast<char*>(const_cast<void*>(a.p));
+    P.out[k].ld = a.ld;
+    P.out[k].plane = a.plane;
+    P.out[k].batch = a.stride;
+    return block_map(o, &P.o[k], a, &P.out[k].tma);
+}
+bool set_in(scalecom_ops* o, TcParams& P, const Surface& a) {
+    P.in = a.p;
+    P.in_ld = a.ld;
+    P.in_plane = a.plane;
+    P.in_batch = a.stride;
+    return block_map(o, &P.i, a, &P.in_tma);
+}
+
 struct Product {
     const Operand *a = nullptr, *b = nullptr, *a2 = nullptr, *b2 = nullptr;   // second pair: GATE's up weights (b2), or a second product
     bool a_mn = false, b_mn = false, a_batched = false, b_batched = false, bf16 = false;
@@ -197,31 +252,38 @@ struct Product {
     int batch = 1;
 };
 
-struct Plan { int bn, splits; int64_t mt, nt, tiles; };
+struct Plan { int bn, cg, splits; int64_t mt, nt, tiles; };
 
-// Tiles and parts of k. A part of one 64-wide block of k costs about 512 cycles of the tensor core with 256-wide tiles and, bound by
-// shared memory and issue, about 320 with 128-wide ones; a split part costs its accumulators' way through L2.
+// Tile shape and parts of k: the least estimated time. A tile's 64 k take the tensor core (256 cycles for 128 columns, three
+// times that for two planes) or the SM's 64 bytes a clock from L2, whichever is longer; what a tile adds at its end is only
+// seen once, behind the last wave; a split part costs its accumulators' way through L2.
 Plan make_plan(const scalecom_ops* o, int epi, int planes, int64_t m, int64_t n, int64_t iters, int64_t batch) {
+    struct Shape { int bn, cg; };
+    static const Shape one[] = {{256, 2}, {128, 2}, {128, 1}}, two[] = {{128, 2}, {128, 1}};
     Plan best = {};
     double least = 1e300;
-    for (int bn = planes > 1 ? 128 : 256; bn >= 128; bn /= 2) {      // two planes: the sums take too many registers for 256
+    for (int i = 0; i < (planes > 1 ? 2 : 3); ++i) {
+        const Shape t = planes > 1 ? two[i] : one[i];
+        const int bm = TC_BM * t.cg;
         Plan p;
-        p.bn = bn;
-        p.mt = ceil_div(m, TC_BM);
-        p.nt = ceil_div(n, epi == EPI_GATE ? bn / 2 : bn);
+        p.bn = t.bn;
+        p.cg = t.cg;
+        p.mt = ceil_div(m, bm);
+        p.nt = ceil_div(n, epi == EPI_GATE ? t.bn / 2 : t.bn);
         p.tiles = p.mt * p.nt;
         if (epi == EPI_GRAM || epi == EPI_POLY) {
             p.tiles = 0;
-            for (int64_t i = 0; i < p.mt; ++i) {
-                const int64_t c = (i * TC_BM + TC_BM - 1) / bn + 1;
+            for (int64_t j = 0; j < p.mt; ++j) {
+                const int64_t c = (j * bm + bm - 1) / t.bn + 1;
                 p.tiles += c < p.nt ? c : p.nt;
             }
         }
-        const double block = planes > 1 ? 1000.0 : bn == 256 ? 512.0 : 320.0, drain = bn * 6.0;
+        const double math = t.bn * 2.0 * (planes > 1 ? 3.0 : 1.0), bytes = planes * (16384.0 + t.bn / t.cg * 128.0);
+        const double block = math > bytes / 64.0 ? math : bytes / 64.0, drain = t.bn * 12.0;
         for (int s = 1; s <= 32 && (s == 1 || s * 2 <= iters); ++s) {
-            if (s > 1 && p.tiles * batch > MAX_SPLIT_TILES) break;
-            const double waves = double(ceil_div(p.tiles * batch * s, o->sms));
-            const double cost = waves * double(ceil_div(iters, s)) * block + drain + (s > 1 ? (waves + s) * bn * 5.0 + 2000.0 : 0.0);
+            if (s > 1 && p.tiles * batch * t.cg > MAX_SPLIT_TILES) break;
+            const double waves = double(ceil_div(p.tiles * batch * s, o->sms / t.cg));
+            const double cost = waves * double(ceil_div(iters, s)) * block + drain + (s > 1 ? (waves + s) * t.bn * 5.0 + 2000.0 : 0.0);
             if (cost < least * 0.97) {
                 least = cost;
                 best = p;
@@ -236,36 +298,43 @@ int64_t product_iters(const Product& p) {
     return ceil_div(p.k, TC_BK) * (p.a2 ? 2 : 1);
 }
 
-template <int BN, int EPI, int PL>
+template <int BN, int EPI, int PL, int CG>
 cudaError_t tc_launch(scalecom_ops* o, const TcParams& P) {
-    const int64_t units = int64_t(P.batch) * P.tiles * P.splits;
-    return launch(o, tc_product_kernel<BN, EPI, PL>, dim3(unsigned(units < o->sms ? units : o->sms)), TC_THREADS, TcShape<BN, PL>::SMEM, P);
+    const int64_t units = int64_t(P.batch) * P.tiles * P.splits, slots = o->sms / CG;
+    return launch_cluster(o, CG, tc_product_kernel<BN, EPI, PL, CG>, dim3(unsigned((units < slots ? units : slots) * CG)), TC_THREADS,
+                          TcShape<BN, EPI, PL, CG>::SMEM, P);
 }
 template <int EPI>
-cudaError_t tc_launch_any(scalecom_ops* o, int bn, int planes, const TcParams& P) {
-    if (planes > 1) return tc_launch<128, EPI, 2>(o, P);
-    return bn == 256 ? tc_launch<256, EPI, 1>(o, P) : tc_launch<128, EPI, 1>(o, P);
+cudaError_t tc_launch_any(scalecom_ops* o, const Plan& pl, int planes, const TcParams& P) {
+    if (planes > 1) return pl.cg == 2 ? tc_launch<128, EPI, 2, 2>(o, P) : tc_launch<128, EPI, 2, 1>(o, P);
+    if (pl.cg == 1) return tc_launch<128, EPI, 1, 1>(o, P);
+    return pl.bn == 256 ? tc_launch<256, EPI, 1, 2>(o, P) : tc_launch<128, EPI, 1, 2>(o, P);
+}
+template <int BN, int EPI, int PL, int CG>
+cudaError_t tc_attribute() {
+    return cudaFuncSetAttribute(tc_product_kernel<BN, EPI, PL, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, EPI, PL, CG>::SMEM);
 }
 template <int EPI>
 cudaError_t tc_attributes() {
-    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    cudaError_t e = cudaFuncSetAttribute(tc_product_kernel<256, EPI, 1>, attr, TcShape<256, 1>::SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_product_kernel<128, EPI, 1>, attr, TcShape<128, 1>::SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(tc_product_kernel<128, EPI, 2>, attr, TcShape<128, 2>::SMEM);
+    cudaError_t e = tc_attribute<256, EPI, 1, 2>();
+    if (e == cudaSuccess) e = tc_attribute<128, EPI, 1, 2>();
+    if (e == cudaSuccess) e = tc_attribute<128, EPI, 1, 1>();
+    if (e == cudaSuccess) e = tc_attribute<128, EPI, 2, 2>();
+    if (e == cudaSuccess) e = tc_attribute<128, EPI, 2, 1>();
     return e;
 }
 
 // Scratch of a split product. Calls run one after another on the stream, so they share it.
 size_t split_bytes(const scalecom_ops* o, int epi, const Product& p) {
     const Plan pl = make_plan(o, epi, p.a->planes, p.m, p.n, product_iters(p), p.batch);
-    return pl.splits > 1 ? size_t(pl.tiles) * p.batch * pl.splits * TC_BM * pl.bn * 4 : 0;
+    return pl.splits > 1 ? size_t(pl.tiles) * p.batch * pl.splits * pl.cg * TC_BM * pl.bn * 4 : 0;
 }
 
 // P: the epilogue's fields are set by the caller
 int run_product(scalecom_ops* o, int epi, const Product& p, TcParams& P, float* partial) {
     const Plan pl = make_plan(o, epi, p.a->planes, p.m, p.n, product_iters(p), p.batch);
     if (pl.tiles * p.batch > 0x7FFFFFFFll / 32) return SCALECOM_ERR_INVALID_ARG;
-    const int bbox = epi == EPI_GATE ? pl.bn / 2 : pl.bn;
+    const int bbox = epi == EPI_GATE ? pl.bn / 2 : pl.bn / pl.cg;      // rows of B that one copy brings
     bool ok = encode(o, &P.a[0], *p.a, p.bf16, p.a_mn, TC_BM) && encode(o, &P.b[0], *p.b, p.bf16, p.b_mn, bbox);
     if (ok && p.a2) ok = encode(o, &P.a[1], *p.a2, p.bf16, p.a_mn, TC_BM);
     if (ok && p.b2) ok = encode(o, &P.b[1], *p.b2, p.bf16, p.b_mn, bbox);
@@ -285,7 +354,7 @@ int run_product(scalecom_ops* o, int epi, const Product& p, TcParams& P, float* 
     P.b_batched = p.b_batched;
     // fp32 accumulators; both operands fp16 (0) or bf16 (1); majors; N / 8, M / 16
     P.idesc = (1u << 4) | ((p.bf16 ? 1u : 0u) << 7) | ((p.bf16 ? 1u : 0u) << 10) | ((p.a_mn ? 1u : 0u) << 15) |
-              ((p.b_mn ? 1u : 0u) << 16) | (uint32_t(pl.bn / 8) << 17) | (uint32_t(TC_BM / 16) << 24);
+              ((p.b_mn ? 1u : 0u) << 16) | (uint32_t(pl.bn / 8) << 17) | (uint32_t(TC_BM * pl.cg / 16) << 24);
     P.status = o->ctrl;
     P.partial = partial;
     P.arrived = o->ctrl + 16;
@@ -293,12 +362,12 @@ int run_product(scalecom_ops* o, int epi, const Product& p, TcParams& P, float* 
     P.amax_b = p.b->amax;
     cudaError_t e;
     switch (epi) {
-        case EPI_STORE: e = tc_launch_any<EPI_STORE>(o, pl.bn, p.a->planes, P); break;
-        case EPI_GATE: e = tc_launch_any<EPI_GATE>(o, pl.bn, p.a->planes, P); break;
-        case EPI_GATE_BWD: e = tc_launch_any<EPI_GATE_BWD>(o, pl.bn, p.a->planes, P); break;
-        case EPI_GRAM: e = tc_launch_any<EPI_GRAM>(o, pl.bn, p.a->planes, P); break;
-        case EPI_POLY: e = tc_launch_any<EPI_POLY>(o, pl.bn, p.a->planes, P); break;
-        default: e = tc_launch_any<EPI_PLANES>(o, pl.bn, p.a->planes, P); break;
+        case EPI_STORE: e = tc_launch_any<EPI_STORE>(o, pl, p.a->planes, P); break;
+        case EPI_GATE: e = tc_launch_any<EPI_GATE>(o, pl, p.a->planes, P); break;
+        case EPI_GATE_BWD: e = tc_launch_any<EPI_GATE_BWD>(o, pl, p.a->planes, P); break;
+        case EPI_GRAM: e = tc_launch_any<EPI_GRAM>(o, pl, p.a->planes, P); break;
+        case EPI_POLY: e = tc_launch_any<EPI_POLY>(o, pl, p.a->planes, P); break;
+        default: e = tc_launch_any<EPI_PLANES>(o, pl, p.a->planes, P); break;
     }
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -392,9 +461,14 @@ int ffn_forward(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* s
         P.type = A.type;
         P.act = A.act;
         P.alpha = 1.0f;
-        P.out = h;
-        P.ldo = fp;
-        P.out2 = saved;
+        Surface hs, ss;
+        hs.p = h; hs.type = A.type; hs.rows = T; hs.cols = f; hs.ld = fp;
+        bool ok = set_out(o, P, 0, hs);
+        if (saved) {
+            ss.p = saved; ss.type = A.type; ss.rows = T; ss.cols = f; ss.ld = f; ss.planes = 2; ss.plane = T * f;
+            ok = ok && set_out(o, P, 1, ss);
+        }
+        if (!ok) return SCALECOM_ERR_CUDA;
         P.amax_o = f32 ? am + AM_H : nullptr;
         rc = run_product(o, EPI_GATE, up, P, partial);
         if (rc == SCALECOM_OK) rc = prep_h.run(o, false);
@@ -402,8 +476,9 @@ int ffn_forward(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* s
         std::memset(&P, 0, sizeof P);
         P.type = A.type;
         P.alpha = 1.0f;
-        P.out = y;
-        P.ldo = ldy;
+        Surface ys;
+        ys.p = y; ys.type = A.type; ys.rows = T; ys.cols = d; ys.ld = ldy;
+        if (!set_out(o, P, 0, ys)) return SCALECOM_ERR_CUDA;
         return run_product(o, EPI_STORE, down, P, partial);
     }
     return SCALECOM_ERR_INTERNAL;
@@ -471,25 +546,23 @@ int ffn_backward(scalecom_ops* o, const FfnArgs& A, int wgrad_type, const void* 
         P.type = A.type;
         P.act = A.act;
         P.alpha = 1.0f;
-        P.in1 = saved;
-        P.in2 = static_cast<const char*>(saved) + T * f * e;
-        P.ldi = f;
-        P.out = mid;
-        P.out2 = mid + T * fp * e;
-        P.out3 = mid + 2 * T * fp * e;
-        P.ldo = fp;
+        Surface ss, ms;
+        ss.p = saved; ss.type = A.type; ss.rows = T; ss.cols = f; ss.ld = f; ss.planes = 2; ss.plane = T * f;
+        ms.p = mid; ms.type = A.type; ms.rows = T; ms.cols = f; ms.ld = fp; ms.planes = 3; ms.plane = T * fp;
+        if (!set_in(o, P, ss) || !set_out(o, P, 0, ms)) return SCALECOM_ERR_CUDA;
         P.amax_o = f32 ? am + AM_DGU : nullptr;
         P.amax_o2 = f32 ? am + AM_H : nullptr;
         rc = run_product(o, EPI_GATE_BWD, pdh, P, partial);
         if (rc == SCALECOM_OK) rc = prep_mid.run(o, false);
         if (rc != SCALECOM_OK) return rc;
-        auto store = [&](const Product& p, void* out, int type, int64_t ld) {
+        auto store = [&](const Product& p, void* out, int type, int64_t ld) -> int {
             TcParams Q;
             std::memset(&Q, 0, sizeof Q);
             Q.type = type;
             Q.alpha = 1.0f;
-            Q.out = out;
-            Q.ldo = ld;
+            Surface os;
+            os.p = out; os.type = type; os.rows = p.m; os.cols = p.n; os.ld = ld;
+            if (!set_out(o, Q, 0, os)) return SCALECOM_ERR_CUDA;
             return run_product(o, EPI_STORE, p, Q, partial);
         };
         if (dx) rc = store(pdx, dx, A.type, lddx);
@@ -602,29 +675,26 @@ int orthogonalise(scalecom_ops* o, const NsArgs& A) {
             std::memset(&P, 0, sizeof P);
             gram.a = gram.b = now;
             P.alpha = float(1.0 / NS_SCALE);
-            P.planes_out = const_cast<__half*>(static_cast<const __half*>(g.p));
-            P.plane_out = g.plane; P.ostride = g.stride; P.ldo = lda;
+            if (!set_out(o, P, 0, surface(g))) return SCALECOM_ERR_CUDA;
             int rc = run_product(o, EPI_GRAM, gram, P, partial);
             if (rc != SCALECOM_OK) return rc;
             std::memset(&P, 0, sizeof P);
             P.poly_a = float(co[0] * NS_SCALE); P.poly_b = co[1]; P.poly_c = float(co[2] / NS_SCALE);
-            P.planes_in = static_cast<const __half*>(g.p);
-            P.plane_in = g.plane;
-            P.planes_out = const_cast<__half*>(static_cast<const __half*>(q.p));
-            P.plane_out = q.plane; P.ostride = q.stride; P.ldo = lda;
+            if (!set_in(o, P, surface(g)) || !set_out(o, P, 0, surface(q))) return SCALECOM_ERR_CUDA;
             rc = run_product(o, EPI_POLY, poly, P, partial);
             if (rc != SCALECOM_OK) return rc;
             std::memset(&P, 0, sizeof P);
             (tall ? apply.a : apply.b) = now;
             if (s + 1 < A.steps) {
                 P.alpha = float(1.0 / NS_SCALE);
-                P.planes_out = const_cast<__half*>(static_cast<const __half*>(next->p));
-                P.plane_out = next->plane; P.ostride = next->stride; P.ldo = ldx;
+                if (!set_out(o, P, 0, surface(*next))) return SCALECOM_ERR_CUDA;
                 rc = run_product(o, EPI_PLANES, apply, P, partial);
             } else {
                 P.alpha = float(double(A.scale) / (NS_SCALE * NS_SCALE));
                 P.type = A.out_type;
-                P.out = A.out; P.ldo = A.ld_out; P.ostride = A.out_stride;
+                Surface os;
+                os.p = A.out; os.type = A.out_type; os.rows = A.rows; os.cols = A.cols; os.ld = A.ld_out; os.batch = int(B); os.stride = A.out_stride;
+                if (!set_out(o, P, 0, os)) return SCALECOM_ERR_CUDA;
                 rc = run_product(o, EPI_STORE, apply, P, partial);
             }
             if (rc != SCALECOM_OK) return rc;

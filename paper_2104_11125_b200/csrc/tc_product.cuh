@@ -5,6 +5,16 @@
 // Newton-Schulz iteration.  Either operand may be stored with k contiguous ("K-major") or with its own rows contiguous
 // ("MN-major"), so no operand is ever transposed in memory.
 //
+// CG = 2: a cluster of two blocks (the two SMs of a TPC) computes a tile of 256 x BN.  Each block holds 128 rows of A and half of the
+// columns' B, and one tcgen05.mma of the first block reads both halves.  An SM takes at most 64 bytes a clock from L2; a
+// single block's 128 x 256 tile asks for 96 while the tensor core runs at its full rate (measured: 800 cycles for a block of 64 k
+// that the tensor core does in 512), the pair's for 64.
+//
+// Results leave through shared memory: a warp lays 32 rows x 32 columns out there and one TMA store writes them, whole sectors at
+// a time.  (Stored from the registers, 16 bytes of 32 different rows at a time, a 128 x 128 tile with three outputs took 17,000
+// cycles, more than the products before it; through TMA about 4,000.)  Rows off the 16-byte grid go out of the same
+// staging area element by element, consecutive lanes on consecutive addresses.
+//
 // Roles (12 warps): warp 0 issues the TMA copies, warp 1 issues tcgen05.mma, warp 2 owns the TMEM allocation, warps 4-11 run
 // the epilogue.  Two accumulators in TMEM: the epilogue of a tile runs under the products of the next.
 //
@@ -26,15 +36,27 @@ constexpr int TC_EPI_WARPS = 8;
 constexpr int TC_EPI_THREADS = TC_EPI_WARPS * 32;
 constexpr int TC_A_BYTES = TC_BM * TC_BK * 2;
 
-template <int BN, int PL> struct TcShape {
-    static constexpr int B_BYTES = BN * TC_BK * 2;
+constexpr int TC_RING = 8192;         // staging area of an epilogue warp: four 32 x 32 blocks of 16 bits, or two of 32
+
+template <int BN, int EPI, int PL, int CG> struct TcShape {
+    static constexpr int B_BYTES = BN / CG * TC_BK * 2;
     static constexpr int STAGE_BYTES = PL * (TC_A_BYTES + B_BYTES);  // A planes, then B planes
-    static constexpr int STAGES = 196608 / STAGE_BYTES;              // 192 KB of operands in flight
-    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;         // + alignment of the swizzle atoms
+    static constexpr bool LOADS = PL == 1 && (EPI == 2 || EPI == 4); // epilogues that read through TMA: 4 KB a warp
+    static constexpr int IN_BYTES = LOADS ? 4096 : 0;
+    static constexpr int EPI_BYTES = TC_EPI_WARPS * (TC_RING + IN_BYTES);
+    static constexpr int STAGES = (227 * 1024 - 1024 - 512 - EPI_BYTES) / STAGE_BYTES;
+    static constexpr int BM = TC_BM * CG;                            // rows of a tile
+    static constexpr int SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 1024;         // + alignment of the swizzle atoms
     static constexpr int TMEM_COLS = 2 * BN;
 };
 
 enum TcEpilogue { EPI_STORE = 0, EPI_GATE = 1, EPI_GATE_BWD = 2, EPI_GRAM = 3, EPI_POLY = 4, EPI_PLANES = 5 };
+
+struct TcOut {
+    char* base;
+    int64_t ld, plane, batch;                 // elements
+    int32_t tma;                              // 16-byte grid: through the tensor map
+};
 
 struct TcParams {
     CUtensorMap a[2], b[2];
@@ -45,22 +67,20 @@ struct TcParams {
     int32_t a_mn, b_mn, a_batched, b_batched;
     uint32_t idesc;
     uint32_t* status;
-    float* partial;                           // splits > 1: [batch*tiles][splits][128][BN] accumulators
-    uint32_t* arrived;                        // splits > 1: [batch*tiles], zero between launches
+    float* partial;                           // splits > 1: [batch*tiles][blocks of a tile][splits][BN][128] accumulators
+    uint32_t* arrived;                        // splits > 1: [batch*tiles][blocks of a tile], zero between launches
 
     // epilogue
-    int32_t type;                             // element type of out / h / saved
+    CUtensorMap o[2], i;                      // outputs and input in blocks of 32 x 32
+    TcOut out[2];                             // STORE: out; GATE: h, saved; GATE_BWD: {dg, du, h}; Newton-Schulz: planes
+    const void* in;                           // GATE_BWD: saved; POLY: the planes of A
+    int64_t in_ld, in_plane, in_batch;
+    int32_t in_tma;
+    int32_t type;                             // element type of the outputs and of saved
     int32_t act;
     float alpha;
     const uint32_t *amax_a, *amax_b;          // largest magnitudes behind the operands' scales, NULL: unscaled
-    void *out, *out2, *out3;                  // STORE: out; GATE: h, saved; GATE_BWD: dg, du, h
-    const void *in1, *in2;                    // GATE_BWD: saved g, u
-    int64_t ldo, ostride;                     // row distance and matrix distance of the outputs (elements)
-    int64_t ldi;                              // row distance of in1, in2 / of saved
     uint32_t *amax_o, *amax_o2;               // fp32 intermediates: their largest magnitude is collected
-    __half* planes_out;                       // Newton-Schulz: [batch][planes][rows][ldo]
-    const __half* planes_in;
-    int64_t plane_out, plane_in;              // distance of the lo plane (elements); 0: hi only
     float poly_a, poly_b, poly_c;
 };
 
@@ -110,19 +130,50 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
         }
     }
 }
+// an address of this block's shared memory as the same place in block `rank` of the cluster
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// CG = 2: `bar` is the first block's barrier (a cluster address), the destination this block's own memory
+template <int CG>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+    if (CG == 2)
+        asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+template <int CG>
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    if (CG == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// arrives at `bar` of every block of the pair when the products issued so far are done
+template <int CG>
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"(uint16_t(3)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tc_ld32(uint32_t addr, float (&v)[32]) {
     uint32_t r[32];
@@ -140,6 +191,34 @@ __device__ __forceinline__ void tc_ld32(uint32_t addr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];"
+                 ::"l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(src) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void sts16(uint32_t at, uint16_t v) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(v) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint16_t lds16(uint32_t at) {
+    uint16_t v;
+    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
 // Shared-memory matrix descriptors, 128-byte swizzle (layout code 2, version 1).
 //   K-major:  a tile is rows of 128 bytes; 8 rows form an atom, atoms 1024 bytes apart.
 //   MN-major: a tile is 64-row-wide panels; in a panel each k is a 128-byte row, 8 k form an atom (1024 bytes
@@ -150,51 +229,70 @@ __device__ __forceinline__ uint64_t tc_desc(uint32_t addr, int mn) {
 }
 
 // ---- activations --------------------------------------------------------------------------------------
-__device__ __forceinline__ float act_value(int act, float g) {
-    switch (act) {
-        case SCALECOM_ACT_SILU: return g / (1.0f + expf(-g));
-        case SCALECOM_ACT_GELU: return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
-        case SCALECOM_ACT_GELU_TANH: return 0.5f * g * (1.0f + tanhf(0.79788456080286536f * (g + 0.044715f * g * g * g)));
-        default: return g > 0.0f ? g : (g == g ? 0.0f : g);
-    }
+// EXACT: CUDA's accurate exp and division, for fp32 results; else the fast ones (about 2^-21 relative), far below a 16-bit rounding.
+template <bool EXACT> __device__ __forceinline__ float act_sigmoid(float g) {
+    return EXACT ? 1.0f / (1.0f + expf(-g)) : __fdividef(1.0f, 1.0f + __expf(-g));
 }
 // value and derivative
-__device__ __forceinline__ void act_both(int act, float g, float& a, float& s) {
-    switch (act) {
-        case SCALECOM_ACT_SILU: {
-            const float p = 1.0f / (1.0f + expf(-g));
-            a = g * p;
-            s = p * (1.0f + g * (1.0f - p));
-            return;
-        }
-        case SCALECOM_ACT_GELU: {
-            const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
-            a = g * c;
-            s = c + g * expf(-0.5f * g * g) * 0.39894228040143268f;
-            return;
-        }
-        case SCALECOM_ACT_GELU_TANH: {
-            if (fabsf(g) > 30.0f) {                 // tanh is +-1 there; the cube below could overflow
-                a = g > 0.0f ? g : 0.0f;
-                s = g > 0.0f ? 1.0f : 0.0f;
-                return;
-            }
-            const float t = tanhf(0.79788456080286536f * (g + 0.044715f * g * g * g));
-            a = 0.5f * g * (1.0f + t);
-            s = 0.5f * (1.0f + t) + 0.5f * g * (1.0f - t * t) * 0.79788456080286536f * (1.0f + 0.134145f * g * g);
-            return;
-        }
-        default:
-            a = g > 0.0f ? g : (g == g ? 0.0f : g);
+template <int ACT, bool EXACT>
+__device__ __forceinline__ void act_both(float g, float& a, float& s) {
+    if (ACT == SCALECOM_ACT_SILU) {
+        // the fast division gives 0 for denominators beyond 2^126, which is the limit here
+        const float p = act_sigmoid<EXACT>(g);
+        a = g * p;
+        s = p * (1.0f + g * (1.0f - p));
+    } else if (ACT == SCALECOM_ACT_GELU) {
+        const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
+        a = g * c;
+        s = c + g * (EXACT ? expf(-0.5f * g * g) : __expf(-0.5f * g * g)) * 0.39894228040143268f;
+    } else if (ACT == SCALECOM_ACT_GELU_TANH) {
+        if (fabsf(g) > 30.0f) {                 // tanh is +-1 there; the cube below could overflow
+            a = g > 0.0f ? g : 0.0f;
             s = g > 0.0f ? 1.0f : 0.0f;
             return;
+        }
+        const float t = tanhf(0.79788456080286536f * (g + 0.044715f * g * g * g));
+        a = 0.5f * g * (1.0f + t);
+        s = 0.5f * (1.0f + t) + 0.5f * g * (1.0f - t * t) * 0.79788456080286536f * (1.0f + 0.134145f * g * g);
+    } else {
+        a = g > 0.0f ? g : (g == g ? 0.0f : g);
+        s = g > 0.0f ? 1.0f : 0.0f;
     }
 }
+// 32 columns at once, so that the choice of the activation is made once and not for each element
+template <int ACT, bool EXACT>
+__device__ __forceinline__ void gate_row(const float (&g)[32], float (&v)[32], const float (&w)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float a, s;
+        act_both<ACT, EXACT>(g[i], a, s);
+        v[i] = a * w[i];
+    }
+}
+template <int ACT, bool EXACT>
+__device__ __forceinline__ void gate_back_row(float (&g)[32], float (&v)[32], float (&w)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float a, s;
+        act_both<ACT, EXACT>(g[i], a, s);
+        const float dh = v[i], u = w[i];
+        g[i] = dh * u * s;             // dg
+        w[i] = dh * a;                 // du
+        v[i] = a * u;                  // h
+    }
+}
+#define SC_FOR_ACT(act, CALL)                                      \
+    switch (act) {                                                 \
+        case SCALECOM_ACT_SILU: CALL(SCALECOM_ACT_SILU); break;    \
+        case SCALECOM_ACT_GELU: CALL(SCALECOM_ACT_GELU); break;    \
+        case SCALECOM_ACT_GELU_TANH: CALL(SCALECOM_ACT_GELU_TANH); break; \
+        default: CALL(SCALECOM_ACT_RELU); break;                   \
+    }
 
 // ---- tile order ----------------------------------------------------------------------------------------
 struct TcUnit { int batch, mt, nt, split, tile; };
 
-template <int BN, int EPI>
+template <int BN, int EPI, int BM>
 __device__ __forceinline__ TcUnit tc_unit(const TcParams& P, int u) {
     TcUnit r;
     r.split = u % P.splits;
@@ -205,15 +303,15 @@ __device__ __forceinline__ TcUnit tc_unit(const TcParams& P, int u) {
     if (EPI == EPI_GRAM || EPI == EPI_POLY) {     // symmetric result: tiles that touch the lower triangle
         int mt = 0;
         for (;; ++mt) {
-            int cols = (mt * TC_BM + TC_BM - 1) / BN + 1;
+            int cols = (mt * BM + BM - 1) / BN + 1;
             if (cols > P.nt) cols = P.nt;
             if (t < cols) break;
             t -= cols;
         }
         r.mt = mt;
         r.nt = t;
-    } else {                                      // bands of 16 row tiles, column by column: the band's A stays in L2
-        constexpr int BAND = 16;
+    } else {                                      // bands of 2048 rows, column by column: the band's A stays in L2
+        constexpr int BAND = 2048 / BM;
         const int band = t / (BAND * P.nt), first = band * BAND;
         const int rows = P.mt - first < BAND ? P.mt - first : BAND;
         const int in = t - band * BAND * P.nt;
@@ -223,115 +321,246 @@ __device__ __forceinline__ TcUnit tc_unit(const TcParams& P, int u) {
     return r;
 }
 
-// ---- epilogues on 32 columns of a row --------------------------------------------------------------------
-__device__ __forceinline__ void store_typed(int type, void* base, int64_t off, const float* v, int ncols) {
-    if (type == SCALECOM_BF16) store_row32(static_cast<__nv_bfloat16*>(base) + off, v, ncols);
-    else if (type == SCALECOM_F16) store_row32(static_cast<__half*>(base) + off, v, ncols);
-    else store_row32(static_cast<float*>(base) + off, v, ncols);
+// ---- blocks of 32 x 32 on their way out and in ----------------------------------------------------------------
+// A lane holds a row.  In the staging area rows are 64 bytes (16-bit types) or 128 (fp32), their 16-byte pieces
+// permuted as the 64- and 128-byte swizzles of the tensor maps have it, so lanes that write the same piece of
+// different rows hit different banks.
+struct Ring {
+    uint32_t base;
+    int n;
+};
+__device__ __forceinline__ uint32_t piece16(uint32_t row, uint32_t piece) { return row * 64u + ((piece ^ ((row >> 1) & 3u)) << 4); }
+__device__ __forceinline__ uint32_t piece32(uint32_t row, uint32_t piece) { return row * 128u + ((piece ^ (row & 7u)) << 4); }
+
+// the next free block of the ring; at most its own size in blocks are still being read by the stores issued before
+template <int BYTES>
+__device__ __forceinline__ uint32_t ring_next(Ring& r) {
+    constexpr int SLOTS = BYTES == 2 ? 4 : 2;
+    if (lane_id() == 0) bulk_wait_read<SLOTS - 1>();
+    __syncwarp();
+    return r.base + uint32_t(r.n++ & (SLOTS - 1)) * (TC_RING / SLOTS);
 }
+// a staged block to global memory at (row0, col0)
+template <int BYTES>
+__device__ __forceinline__ void ring_send(const TcParams& P, int k, uint32_t slot, int row0, int col0, int plane, int batch) {
+    const TcOut& o = P.out[k];
+    if (o.tma) {
+        fence_async_smem();
+        __syncwarp();
+        if (lane_id() == 0) {
+            tma_store(&P.o[k], col0, row0, plane, batch, slot);
+            bulk_commit();
+        }
+    } else {
+        __syncwarp();
+        const uint32_t lane = lane_id();
+        const int rows = min(32, P.m - row0);
+        const int64_t at = int64_t(batch) * o.batch + int64_t(plane) * o.plane + int64_t(row0) * o.ld + col0 + lane;
+        if (col0 + int(lane) < P.n) {
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r) {
+                if (BYTES == 2) reinterpret_cast<uint16_t*>(o.base)[at + r * o.ld] = lds16(slot + piece16(r, lane >> 3) + (lane & 7u) * 2);
+                else reinterpret_cast<uint32_t*>(o.base)[at + r * o.ld] = lds32(slot + piece32(r, lane >> 2) + (lane & 3u) * 4);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) bulk_commit();               // an empty group: the ring counts one for each block
+    }
+}
+__device__ __forceinline__ uint32_t pack16(int type, float a, float b) {
+    if (type == SCALECOM_BF16) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&t);
+    }
+    const __half2 t = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ void stage16(uint32_t slot, int type, const float (&v)[32]) {
+    const uint32_t lane = lane_id();
+    uint32_t p[16];
+    if (type == SCALECOM_BF16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = pack16(SCALECOM_BF16, v[2 * i], v[2 * i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = pack16(SCALECOM_F16, v[2 * i], v[2 * i + 1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sts128(slot + piece16(lane, i), p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
+}
+template <bool MAY_F32>
+__device__ __forceinline__ void emit(const TcParams& P, int k, Ring& ring, int type, const float (&v)[32], int row0, int col0, int plane, int batch) {
+    if (MAY_F32 && type == SCALECOM_F32) {
+        const uint32_t slot = ring_next<4>(ring), lane = lane_id();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            sts128(slot + piece32(lane, i), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+        ring_send<4>(P, k, slot, row0, col0, plane, batch);
+    } else {
+        const uint32_t slot = ring_next<2>(ring);
+        stage16(slot, type, v);
+        ring_send<2>(P, k, slot, row0, col0, plane, batch);
+    }
+}
+// fp16 planes of a block, and with MIRROR of its transpose at (col0, row0)
+template <int PL, bool MIRROR>
+__device__ __forceinline__ void emit_planes(const TcParams& P, Ring& ring, float (&v)[32], int row0, int col0, int batch) {
+    const uint32_t lane = lane_id();
+#pragma unroll
+    for (int pl = 0; pl < PL; ++pl) {
+        if (pl == 1) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                __half h, l;
+                split_planes(v[i], h, l);
+                v[i] = __half2float(l);
+            }
+        }
+        emit<false>(P, 0, ring, SCALECOM_F16, v, row0, col0, pl, batch);
+        if (MIRROR && col0 != row0) {
+            const uint32_t slot = ring_next<2>(ring);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                sts16(slot + piece16(i, lane >> 3) + (lane & 7u) * 2, __half_as_ushort(__float2half_rn(v[i])));
+            ring_send<2>(P, 0, slot, col0, row0, pl, batch);
+        }
+    }
+}
+// 32 values of this lane's row, from a block that a TMA load has brought
+__device__ __forceinline__ void take16(uint32_t at, int type, float (&v)[32]) {
+    const uint32_t lane = lane_id();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint4 q = lds128(at + piece16(lane, i));
+        const uint32_t r[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (type == SCALECOM_BF16) {
+                v[8 * i + 2 * j] = __uint_as_float(r[j] << 16);
+                v[8 * i + 2 * j + 1] = __uint_as_float(r[j] & 0xFFFF0000u);
+            } else {
+                const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&r[j]));
+                v[8 * i + 2 * j] = t.x;
+                v[8 * i + 2 * j + 1] = t.y;
+            }
+        }
+    }
+}
+// the same straight from global memory
 __device__ __forceinline__ void load_typed(int type, const void* base, int64_t off, float* v, int ncols) {
     if (type == SCALECOM_BF16) load_row32(static_cast<const __nv_bfloat16*>(base) + off, v, ncols);
     else if (type == SCALECOM_F16) load_row32(static_cast<const __half*>(base) + off, v, ncols);
     else load_row32(static_cast<const float*>(base) + off, v, ncols);
 }
-__device__ __forceinline__ void store_planes(__half* base, int64_t lo, int64_t off, const float* v, int ncols) {
-    if (!lo) {
-        store_row32(base + off, v, ncols);
-        return;
+
+// Blocks that an epilogue reads (GATE_BWD: g and u, POLY: A), one ahead of the block being worked on.
+struct Inflow {
+    uint32_t smem, bar;
+    uint32_t phase;
+    bool pending;
+};
+template <int EPI>
+__device__ __forceinline__ bool block_used(const TcParams& P, int row0, int col0) {
+    return row0 < P.m && col0 < P.n && (!(EPI == EPI_GRAM || EPI == EPI_POLY) || col0 <= row0);
+}
+template <int EPI>
+__device__ __forceinline__ void inflow_start(const TcParams& P, Inflow& f, int row0, int col0, int batch) {
+    if (!P.in_tma || f.pending || !block_used<EPI>(P, row0, col0)) return;
+    f.pending = true;
+    if (lane_id() == 0) {
+        mbar_expect(f.bar, EPI == EPI_GATE_BWD ? 4096u : 2048u);
+        tma_load<1>(f.smem, &P.i, col0, row0, 0, batch, f.bar);
+        if (EPI == EPI_GATE_BWD) tma_load<1>(f.smem + 2048u, &P.i, col0, row0, 1, batch, f.bar);
     }
-    float l[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        __half h, r;
-        split_planes(v[i], h, r);
-        l[i] = __half2float(r);
-    }
-    store_row32(base + off, v, ncols);
-    store_row32(base + lo + off, l, ncols);
 }
 
-template <int EPI>
-__device__ __forceinline__ void tc_epilogue(const TcParams& P, const TcUnit& u, int row, int col, float (&v)[32], float (&w)[32],
-                                            float un, uint32_t& top, uint32_t& top2) {
-    const int nc = P.n - col;
-    if (row >= P.m || nc <= 0) return;
+// ---- epilogues on a block of 32 x 32: v (and w) hold this lane's row --------------------------------------------
+template <int EPI, int PL>
+__device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, int row0, int col0, float (&v)[32], float (&w)[32], float un,
+                                            uint32_t& top, uint32_t& top2, Ring& ring, Inflow& in, volatile uint32_t* abort) {
+    if (!block_used<EPI>(P, row0, col0)) return true;
+    const int row = row0 + int(lane_id()), nc = P.n - col0;
+    const bool inside = row < P.m;
     if (EPI == EPI_STORE) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= un;
-        store_typed(P.type, P.out, int64_t(u.batch) * P.ostride + int64_t(row) * P.ldo + col, v, nc);
+        emit<true>(P, 0, ring, P.type, v, row0, col0, 0, u.batch);
     } else if (EPI == EPI_GATE) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) { v[i] *= un; w[i] *= un; }
-        if (P.out2) {
-            const int64_t at = int64_t(row) * P.n + col;
-            store_typed(P.type, P.out2, at, v, nc);
-            store_typed(P.type, P.out2, at + int64_t(P.m) * P.n, w, nc);
+        if (P.out[1].base) {
+            emit<PL == 2>(P, 1, ring, P.type, v, row0, col0, 0, 0);
+            emit<PL == 2>(P, 1, ring, P.type, w, row0, col0, 1, 0);
         }
+#define SC_CALL(ACT) gate_row<ACT, PL == 2>(v, v, w)
+        SC_FOR_ACT(P.act, SC_CALL)
+#undef SC_CALL
+        if (PL == 2 && inside) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            v[i] = act_value(P.act, v[i]) * w[i];
-            if (i < nc) top = max(top, finite_bits(v[i]));
+            for (int i = 0; i < 32; ++i)
+                if (i < nc) top = max(top, finite_bits(v[i]));
         }
-        store_typed(P.type, P.out, int64_t(row) * P.ldo + col, v, nc);
+        emit<PL == 2>(P, 0, ring, P.type, v, row0, col0, 0, 0);
     } else if (EPI == EPI_GATE_BWD) {
         float g[32];
-        const int64_t at = int64_t(row) * P.ldi + col;
-        load_typed(P.type, P.in1, at, g, nc);
-        load_typed(P.type, P.in2, at, w, nc);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            float a, s;
-            act_both(P.act, g[i], a, s);
-            const float dh = v[i] * un, uu = w[i];
-            g[i] = dh * uu * s;            // dg
-            w[i] = dh * a;                 // du
-            v[i] = a * uu;                 // h
-            if (i < nc) {
-                top = max(top, max(finite_bits(g[i]), finite_bits(w[i])));
-                top2 = max(top2, finite_bits(v[i]));
-            }
+        if (PL == 1 && P.in_tma) {
+            if (!__all_sync(FULL, mbar_wait(in.bar, in.phase, abort, P.status))) return false;
+            in.phase ^= 1u;
+            in.pending = false;
+            take16(in.smem, P.type, g);
+            take16(in.smem + 2048u, P.type, w);
+            __syncwarp();
+        } else {
+            const int64_t at = int64_t(row) * P.in_ld + col0;
+            load_typed(P.type, P.in, at, g, inside ? nc : 0);
+            load_typed(P.type, P.in, at + P.in_plane, w, inside ? nc : 0);
         }
-        const int64_t to = int64_t(row) * P.ldo + col;
-        store_typed(P.type, P.out, to, g, nc);
-        store_typed(P.type, P.out2, to, w, nc);
-        store_typed(P.type, P.out3, to, v, nc);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= un;
+#define SC_CALL(ACT) gate_back_row<ACT, PL == 2>(g, v, w)
+        SC_FOR_ACT(P.act, SC_CALL)
+#undef SC_CALL
+        if (PL == 2 && inside) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < nc) {
+                    top = max(top, max(finite_bits(g[i]), finite_bits(w[i])));
+                    top2 = max(top2, finite_bits(v[i]));
+                }
+        }
+        emit<PL == 2>(P, 0, ring, P.type, g, row0, col0, 0, 0);
+        emit<PL == 2>(P, 0, ring, P.type, w, row0, col0, 1, 0);
+        emit<PL == 2>(P, 0, ring, P.type, v, row0, col0, 2, 0);
     } else if (EPI == EPI_PLANES) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= P.alpha;
-        store_planes(P.planes_out + int64_t(u.batch) * P.ostride, P.plane_out, int64_t(row) * P.ldo + col, v, nc);
+        emit_planes<PL, false>(P, ring, v, row0, col0, u.batch);
     } else {
-        // symmetric result: columns up to the diagonal, stored at (row, col) and at (col, row)
-        const int valid = min(nc, row - col + 1);
-        if (valid <= 0) return;
-        const int64_t at = int64_t(row) * P.ldo + col;
+        // a symmetric result: blocks up to the diagonal, stored here and mirrored
         if (EPI == EPI_POLY) {
-            const __half* in = P.planes_in + int64_t(u.batch) * P.ostride + at;
-            load_row32(in, w, valid);
-            if (P.plane_in) {
+            if (PL == 1) {
+                if (!__all_sync(FULL, mbar_wait(in.bar, in.phase, abort, P.status))) return false;
+                in.phase ^= 1u;
+                in.pending = false;
+                take16(in.smem, SCALECOM_F16, w);
+                __syncwarp();
+            } else {
+                const int64_t at = int64_t(u.batch) * P.in_batch + int64_t(row) * P.in_ld + col0;
+                load_typed(SCALECOM_F16, P.in, at, w, inside ? nc : 0);
                 float l[32];
-                load_row32(in + P.plane_in, l, valid);
+                load_typed(SCALECOM_F16, P.in, at + P.in_plane, l, inside ? nc : 0);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) w[i] += l[i];
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = P.poly_b * w[i] + P.poly_c * v[i] + (i == row - col ? P.poly_a : 0.0f);
+            for (int i = 0; i < 32; ++i) v[i] = P.poly_b * w[i] + P.poly_c * v[i] + (i == row - col0 ? P.poly_a : 0.0f);
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] *= P.alpha;
         }
-        __half* o = P.planes_out + int64_t(u.batch) * P.ostride;
-        store_planes(o, P.plane_out, at, v, valid);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            if (i < valid) {                       // lanes hold consecutive rows: the mirrored store is coalesced
-                const int64_t mt = int64_t(col + i) * P.ldo + row;
-                __half h, l;
-                split_planes(v[i], h, l);
-                o[mt] = h;
-                if (P.plane_out) o[P.plane_out + mt] = l;
-            }
-        }
+        emit_planes<PL, true>(P, ring, v, row0, col0, u.batch);
     }
+    return true;
 }
 
 // whether `ok` holds for all threads of the epilogue warps (a barrier among them)
@@ -342,11 +571,11 @@ __device__ __forceinline__ bool epilogue_all(bool ok) {
     return r != 0u;
 }
 
-template <int BN, int EPI, int PL>
+template <int BN, int EPI, int PL, int CG>
 __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_constant__ TcParams P) {
-    using S = TcShape<BN, PL>;
+    using S = TcShape<BN, EPI, PL, CG>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t bars[2 * S::STAGES + 4 + 1];
+    __shared__ alignas(8) uint64_t bars[2 * S::STAGES + 4 + 1 + TC_EPI_WARPS];
     __shared__ uint32_t tmem_base, abort_flag, last_flag;
 
     const uint32_t warp = warp_id(), lane = lane_id();
@@ -357,21 +586,30 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
     auto tfull = [&](int s) { return bar0 + 8u * (2 * S::STAGES + s); };
     auto tempty = [&](int s) { return bar0 + 8u * (2 * S::STAGES + 2 + s); };
     const uint32_t drain = bar0 + 8u * (2 * S::STAGES + 4);
+    const uint32_t inflow0 = drain + 8u;
 
     if (warp == 0 && lane == 0) {
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(tfull(s), 1); mbar_init(tempty(s), TC_EPI_WARPS); }
+        for (int s = 0; s < 2; ++s) { mbar_init(tfull(s), 1); mbar_init(tempty(s), TC_EPI_WARPS * CG); }
         mbar_init(drain, 1);
+        for (int w = 0; w < TC_EPI_WARPS; ++w) mbar_init(inflow0 + 8u * w, 1);
         abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(S::TMEM_COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(S::TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(S::TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
+    const uint32_t rank = CG == 2 ? blockIdx.x & 1u : 0u;        // in the cluster, whose size is CG
     tc_fence_before();
     __syncthreads();
+    if (CG == 2) cluster_sync();                                 // the pair's barriers are set up on both sides
     tc_fence_after();
     const uint32_t tmem = tmem_base;
     chain_launch();
@@ -380,51 +618,56 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
     volatile uint32_t* abort = &abort_flag;
     const int units = P.batch * P.tiles * P.splits;
     const int iters = P.pairs * P.kblocks;
+    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
     if (warp == 0) {
         if (lane == 0) {
             int n_issued = 0;                       // copies issued so far; stage and phase follow from it
             bool ok = true;
-            for (int un = blockIdx.x; ok && un < units; un += gridDim.x) {
-                const TcUnit u = tc_unit<BN, EPI>(P, un);
+            for (int un = first; ok && un < units; un += stride) {
+                const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
                 const int it0 = int(int64_t(iters) * u.split / P.splits), it1 = int(int64_t(iters) * (u.split + 1) / P.splits);
-                const int m0 = u.mt * TC_BM, n0 = u.nt * (EPI == EPI_GATE ? BN / 2 : BN);
+                const int m0 = u.mt * S::BM + int(rank) * TC_BM;
+                const int n0 = EPI == EPI_GATE ? u.nt * (BN / 2) : u.nt * BN + int(rank) * (BN / CG);
                 const int ba = P.a_batched ? u.batch : 0, bb = P.b_batched ? u.batch : 0;
                 for (int it = it0; it < it1; ++it, ++n_issued) {
                     const int s = n_issued % S::STAGES, round = n_issued / S::STAGES;
                     if (!mbar_wait(empty(s), (round & 1) ^ 1, abort, P.status)) { ok = false; break; }
                     const int pair = it >= P.kblocks, k0 = (it - pair * P.kblocks) * TC_BK;
-                    const uint32_t a = tiles0 + s * S::STAGE_BYTES, b = a + PL * TC_A_BYTES, bar = full(s);
-                    mbar_expect(bar, S::STAGE_BYTES);
+                    const uint32_t a = tiles0 + s * S::STAGE_BYTES, b = a + PL * TC_A_BYTES;
+                    const uint32_t bar = CG == 2 ? in_block(full(s), 0) : full(s);
+                    if (rank == 0) mbar_expect(full(s), S::STAGE_BYTES * CG);      // both blocks' copies
 #pragma unroll
                     for (int pl = 0; pl < PL; ++pl) {
                         const uint32_t ap = a + pl * TC_A_BYTES, bp = b + pl * S::B_BYTES;
                         if (P.a_mn) {
-                            for (int j = 0; j < TC_BM / 64; ++j) tma_load(ap + j * 8192, &P.a[pair], m0 + 64 * j, k0, pl, ba, bar);
+                            for (int j = 0; j < TC_BM / 64; ++j) tma_load<CG>(ap + j * 8192, &P.a[pair], m0 + 64 * j, k0, pl, ba, bar);
                         } else {
-                            tma_load(ap, &P.a[pair], k0, m0, pl, ba, bar);
+                            tma_load<CG>(ap, &P.a[pair], k0, m0, pl, ba, bar);
                         }
-                        if (EPI == EPI_GATE) {      // gate columns, then the same columns of the up projection
-                            tma_load(bp, &P.b[0], k0, n0, pl, bb, bar);
-                            tma_load(bp + S::B_BYTES / 2, &P.b[1], k0, n0, pl, bb, bar);
+                        if (EPI == EPI_GATE && CG == 2) {       // the pair's first block has the gate columns, the second the up columns
+                            tma_load<CG>(bp, &P.b[rank], k0, n0, pl, bb, bar);
+                        } else if (EPI == EPI_GATE) {
+                            tma_load<CG>(bp, &P.b[0], k0, n0, pl, bb, bar);
+                            tma_load<CG>(bp + S::B_BYTES / 2, &P.b[1], k0, n0, pl, bb, bar);
                         } else if (P.b_mn) {
-                            for (int j = 0; j < BN / 64; ++j) tma_load(bp + j * 8192, &P.b[pair], n0 + 64 * j, k0, pl, bb, bar);
+                            for (int j = 0; j < BN / CG / 64; ++j) tma_load<CG>(bp + j * 8192, &P.b[pair], n0 + 64 * j, k0, pl, bb, bar);
                         } else {
-                            tma_load(bp, &P.b[pair], k0, n0, pl, bb, bar);
+                            tma_load<CG>(bp, &P.b[pair], k0, n0, pl, bb, bar);
                         }
                     }
                 }
             }
-            if (!ok)                                // the copies still in flight write this block's shared memory
+            if (!ok && rank == 0)                   // the copies still in flight write shared memory (the pair's: the first block sees them all)
                 for (int i = n_issued > S::STAGES ? n_issued - S::STAGES : 0; i < n_issued; ++i)
                     mbar_drain(full(i % S::STAGES), (i / S::STAGES) & 1);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             int n_used = 0, n_acc = 0;
             bool ok = true;
-            for (int un = blockIdx.x; ok && un < units; un += gridDim.x, ++n_acc) {
-                const TcUnit u = tc_unit<BN, EPI>(P, un);
+            for (int un = first; ok && un < units; un += stride, ++n_acc) {
+                const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
                 const int it0 = int(int64_t(iters) * u.split / P.splits), it1 = int(int64_t(iters) * (u.split + 1) / P.splits);
                 if (PL == 1) {
                     if (!mbar_wait(tempty(n_acc & 1), ((n_acc >> 1) & 1) ^ 1, abort, P.status)) { ok = false; break; }
@@ -446,15 +689,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                         const uint64_t db = tc_desc(b + (PL == 2 && t == 1 ? S::B_BYTES : 0), P.b_mn);
 #pragma unroll
                         for (int k = 0; k < TC_BK / 16; ++k)
-                            tc_mma(d, da + k * step_a, db + k * step_b, P.idesc, (t > 0 || k > 0 || (PL == 1 && it > it0)) ? 1u : 0u);
+                            tc_mma<CG>(d, da + k * step_a, db + k * step_b, P.idesc, (t > 0 || k > 0 || (PL == 1 && it > it0)) ? 1u : 0u);
                     }
-                    tc_commit(empty(s));
-                    if (PL == 2) tc_commit(tfull(n_used & 1));
+                    tc_commit<CG>(empty(s));
+                    if (PL == 2) tc_commit<CG>(tfull(n_used & 1));
                 }
-                if (PL == 1 && ok) tc_commit(tfull(n_acc & 1));
+                if (PL == 1 && ok) tc_commit<CG>(tfull(n_acc & 1));
             }
             if (!ok) {                              // products in flight read shared memory and write TMEM
-                tc_commit(drain);
+                tc_commit<CG>(drain);
                 mbar_drain(drain, 0);
             }
         }
@@ -465,19 +708,30 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
         // result columns of a tile, and a warp's 32-column chunks of them: GATE works on a gate chunk and the up chunk beside it
         constexpr int WIDTH = EPI == EPI_GATE ? BN / 2 : BN, CHUNKS = WIDTH / 64;
         auto chunk = [&](int c) { return (int(half) * CHUNKS + c) * 32; };
+        auto acc_free = [&](int i) {                // the first block issues the products: it waits for both blocks' warps
+            if (rank == 0) mbar_arrive(tempty(i));
+            else mbar_arrive_cluster(in_block(tempty(i), 0));
+        };
         float un_scale = P.alpha;
         if (P.amax_a) un_scale *= plane_unscale(*P.amax_a) * plane_unscale(*P.amax_b);
         uint32_t top = 0u, top2 = 0u;
         int n_acc = 0;
-        for (int un = blockIdx.x; un < units; un += gridDim.x) {
-            const TcUnit u = tc_unit<BN, EPI>(P, un);
-            const int row = u.mt * TC_BM + quad * 32 + lane;
+        const uint32_t stage0 = tiles0 + S::STAGES * S::STAGE_BYTES;
+        Ring ring = {stage0 + (warp - 4u) * TC_RING, 0};
+        Inflow in = {stage0 + TC_EPI_WARPS * TC_RING + (warp - 4u) * S::IN_BYTES, inflow0 + 8u * (warp - 4u), 0u, false};
+        auto begin = [&](const TcUnit& u, int row0, int c) {
+            if (S::LOADS && c < CHUNKS) inflow_start<EPI>(P, in, row0, u.nt * WIDTH + chunk(c), u.batch);
+        };
+        for (int un = first; un < units; un += stride) {
+            const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
+            const int row0 = u.mt * S::BM + int(rank) * TC_BM + int(quad) * 32;
             float v[32], w[32];
             float sum[PL == 2 ? BN / 64 : 1][32];       // PL = 2: this thread's columns, in the order of `column`
             auto column = [&](int c) {                  // TMEM column of the thread's c-th 32 columns
                 if (EPI == EPI_GATE && PL == 2) return (c & 1) * (BN / 2) + (int(half) * (BN / 128) + (c >> 1)) * 32;
                 return int(half) * (BN / 2) + c * 32;
             };
+            if (P.splits == 1) begin(u, row0, 0);
             bool ok = true;
             uint32_t acc = 0;
             int q = 0;
@@ -501,7 +755,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(tempty(q));
+                    if (lane == 0) acc_free(q);
                 }
             } else {
                 q = n_acc & 1;
@@ -516,12 +770,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 if (PL == 1) {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(tempty(q));
+                    if (lane == 0) acc_free(q);
                 }
             };
             if (P.splits > 1) {
                 // this part's accumulators to scratch, [column][row]; the block that arrives last adds the parts up in their order
-                float* mine = P.partial + (int64_t(u.tile) * P.splits) * (TC_BM * BN) + quad * 32 + lane;
+                const int slot = u.tile * CG + int(rank);
+                float* mine = P.partial + (int64_t(slot) * P.splits) * (TC_BM * BN) + quad * 32 + lane;
                 float* put = mine + int64_t(u.split) * (TC_BM * BN);
                 if (PL == 2) {
 #pragma unroll
@@ -540,9 +795,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 __threadfence();
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (tid == 0) {
-                    const uint32_t before = atomicAdd(&P.arrived[u.tile], 1u);
+                    const uint32_t before = atomicAdd(&P.arrived[slot], 1u);
                     last_flag = before + 1u == uint32_t(P.splits);
-                    if (before + 1u == uint32_t(P.splits)) P.arrived[u.tile] = 0u;
+                    if (before + 1u == uint32_t(P.splits)) P.arrived[slot] = 0u;
                     __threadfence();
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -564,13 +819,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     const int at = chunk(c);
                     gather(at, v);
                     if (EPI == EPI_GATE) gather(BN / 2 + at, w);
-                    tc_epilogue<EPI>(P, u, row, u.nt * WIDTH + at, v, w, un_scale, top, top2);
+                    begin(u, row0, c);
+                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, v, w, un_scale, top, top2, ring, in, abort);
                 }
             } else if (PL == 2) {
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
-                    if (EPI == EPI_GATE) tc_epilogue<EPI>(P, u, row, u.nt * WIDTH + chunk(c), sum[2 * c], sum[2 * c + 1], un_scale, top, top2);
-                    else tc_epilogue<EPI>(P, u, row, u.nt * WIDTH + chunk(c), sum[c], w, un_scale, top, top2);
+                    if (EPI == EPI_GATE) tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + chunk(c), sum[2 * c], sum[2 * c + 1], un_scale, top, top2, ring, in, abort);
+                    else tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + chunk(c), sum[c], w, un_scale, top, top2, ring, in, abort);
                 }
             } else {
 #pragma unroll 1
@@ -579,11 +835,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     tc_ld32(acc + at, v);
                     if (EPI == EPI_GATE) tc_ld32(acc + BN / 2 + at, w);
                     if (c == CHUNKS - 1) release();
-                    tc_epilogue<EPI>(P, u, row, u.nt * WIDTH + at, v, w, un_scale, top, top2);
+                    if (ok) begin(u, row0, c);
+                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, v, w, un_scale, top, top2, ring, in, abort);
+                    if (ok) begin(u, row0, c + 1);
                 }
             }
         }
-        if (EPI == EPI_GATE || EPI == EPI_GATE_BWD) {
+        if (lane == 0) {
+            if (in.pending) mbar_drain(in.bar, in.phase);
+            bulk_wait_all();                        // the staging area is read, and the results are written, before the block ends
+        }
+        if (PL == 2 && (EPI == EPI_GATE || EPI == EPI_GATE_BWD)) {
             if (P.amax_o) {
                 top = __reduce_max_sync(FULL, top);
                 if (lane == 0 && top) atomicMax(P.amax_o, top);
@@ -597,9 +859,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (CG == 2) cluster_sync();                    // neither block leaves while the other may reach its memory
     if (warp == 2) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::TMEM_COLS) : "memory");
+        if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::TMEM_COLS) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::TMEM_COLS) : "memory");
     }
 }
 
