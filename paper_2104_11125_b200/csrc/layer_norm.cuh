@@ -10,6 +10,9 @@ namespace sc {
 
 constexpr int LN_THREADS = 256;
 
+// blocks on a multiprocessor for an estimate of a thread's registers
+constexpr int ln_blocks(int regs) { return regs <= 64 ? 4 : regs <= 80 ? 3 : regs <= 128 ? 2 : 1; }
+
 struct LnParams {
     const void *x, *dy;
     void *y, *dx;
@@ -24,113 +27,7 @@ struct LnParams {
     float eps;
 };
 
-// sum over the TPR threads that share a row; TPR = 32: a warp, TPR = LN_THREADS: the block
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* smem) {
-    v = warp_sum_f(v);
-    if (TPR > 32) {
-        __syncthreads();                                 // the array may still be read from the sum before
-        if (lane_id() == 0) smem[warp_id()] = v;
-        __syncthreads();
-        v = smem[lane_id() & (TPR / 32 - 1)];
-#pragma unroll
-        for (int o = TPR / 64; o; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-    }
-    return v;
-}
-template <int TPR>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2* smem) {
-    a = warp_sum_f(a);
-    b = warp_sum_f(b);
-    if (TPR > 32) {
-        __syncthreads();
-        if (lane_id() == 0) smem[warp_id()] = make_float2(a, b);
-        __syncthreads();
-        const float2 t = smem[lane_id() & (TPR / 32 - 1)];
-        a = t.x;
-        b = t.y;
-#pragma unroll
-        for (int o = TPR / 64; o; o >>= 1) {
-            a += __shfl_xor_sync(FULL, a, o);
-            b += __shfl_xor_sync(FULL, b, o);
-        }
-    }
-    return make_float2(a, b);
-}
-
-template <typename T, int VEC>
-__device__ __forceinline__ void ln_load(const T* p, int col, int width, float (&v)[VEC]) {
-    if (VEC == 1 || col + VEC <= width) {
-        if (VEC > 1 || col < width) load_up<T, VEC>(p + col, v);
-        else v[0] = 0.0f;
-    } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[j] = col + j < width ? Elem<T>::up(p[col + j]) : 0.0f;
-    }
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void ln_store(T* p, int col, int width, const float (&v)[VEC]) {
-    if (VEC == 1 || col + VEC <= width) {
-        if (VEC > 1 || col < width) store_down<T, VEC>(p + col, v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            if (col + j < width) p[col + j] = Elem<T>::down(v[j]);
-    }
-}
-
-template <typename T, int VEC, int NV, int TPR>
-__global__ void __launch_bounds__(LN_THREADS) layer_norm_kernel(const LnParams P) {
-    __shared__ float red[LN_THREADS / 32];
-    constexpr int RPB = LN_THREADS / TPR;
-    const int t = threadIdx.x % TPR;
-    const float inv = 1.0f / float(P.width);
-    chain_launch();
-    chain_wait();
-    for (int64_t row = int64_t(blockIdx.x) * RPB + threadIdx.x / TPR; row < P.rows; row += int64_t(gridDim.x) * RPB) {
-        const T* x = static_cast<const T*>(P.x) + row * P.ldx;
-        float v[NV][VEC];
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) ln_load<T, VEC>(x, (i * TPR + t) * VEC, P.width, v[i]);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) s += v[i][j];
-        const float mean = row_sum<TPR>(s, red) * inv;
-        s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                v[i][j] -= mean;
-                if ((i * TPR + t) * VEC + j < P.width) s += v[i][j] * v[i][j];
-            }
-        const float rstd = 1.0f / sqrtf(row_sum<TPR>(s, red) * inv + P.eps);
-        T* y = static_cast<T*>(P.y) + row * P.ldy;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int col = (i * TPR + t) * VEC;
-            if (col < P.width) {
-                float o[VEC];
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int c = min(col + j, P.width - 1);
-                    const float g = P.gamma ? __ldg(P.gamma + c) : 1.0f, b = P.beta ? __ldg(P.beta + c) : 0.0f;
-                    o[j] = v[i][j] * rstd * g + b;
-                }
-                ln_store<T, VEC>(y, col, P.width, o);
-            }
-        }
-        if (t == 0) {
-            if (P.mean) P.mean[row] = mean;
-            if (P.rstd) P.rstd[row] = rstd;
-        }
-    }
-}
-
-// Rows too long for registers: one pass forms mean and squared differences with Welford's update, the threads' triples
-// are merged pairwise, a second pass (of a row that is then in L2) writes y.
+// Count, mean and sum of squared differences of a set of values; two sets joined (Chan, Golub and LeVeque's pairwise form).
 struct LnMoments { float n, mean, m2; };
 __device__ __forceinline__ LnMoments ln_merge(const LnMoments& a, const LnMoments& b) {
     const float n = a.n + b.n;
@@ -142,6 +39,181 @@ __device__ __forceinline__ LnMoments ln_merge(const LnMoments& a, const LnMoment
     r.m2 = a.m2 + b.m2 + d * d * a.n * f;
     return r;
 }
+
+// Mean and squared differences over the TPR threads of a row (32: a warp, LN_THREADS: the block) from those of each thread's N
+// values: pairs of sets of one size, so the pairwise form has constants only. The same bits in every thread. `part`
+// has two arrays used in turn, so that one barrier a row is enough.
+template <int TPR, int N>
+__device__ __forceinline__ void row_moments(float& mean, float& m2, float2 (*part)[LN_THREADS / 32], int turn) {
+    static_assert(TPR == 32 || TPR == 256, "levels");
+    auto join = [&](int o, float size) {
+        const float d = __shfl_xor_sync(FULL, mean, o) - mean;
+        mean += 0.5f * d;
+        m2 += __shfl_xor_sync(FULL, m2, o) + d * d * (0.5f * size);
+    };
+#pragma unroll
+    for (int l = 0; l < 5; ++l) join(1 << l, float(N << l));
+    if (TPR > 32) {
+        if (lane_id() == 0) part[turn][warp_id()] = make_float2(mean, m2);
+        __syncthreads();
+        const float2 t = part[turn][lane_id() & 7];
+        mean = t.x;
+        m2 = t.y;
+#pragma unroll
+        for (int l = 0; l < 3; ++l) join(1 << l, float(N << (5 + l)));
+    }
+}
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* part) {
+    v = warp_sum_f(v);
+    if (TPR > 32) {
+        if (lane_id() == 0) part[warp_id()] = v;
+        __syncthreads();
+        v = part[lane_id() & (TPR / 32 - 1)];
+#pragma unroll
+        for (int o = TPR / 64; o; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    }
+    return v;
+}
+template <int TPR>
+__device__ __forceinline__ float2 row_sum2(float a, float b, float2 (*part)[LN_THREADS / 32], int turn) {
+    a = warp_sum_f(a);
+    b = warp_sum_f(b);
+    if (TPR > 32) {
+        if (lane_id() == 0) part[turn][warp_id()] = make_float2(a, b);
+        __syncthreads();
+        const float2 t = part[turn][lane_id() & (TPR / 32 - 1)];
+        a = t.x;
+        b = t.y;
+#pragma unroll
+        for (int o = TPR / 64; o; o >>= 1) {
+            a += __shfl_xor_sync(FULL, a, o);
+            b += __shfl_xor_sync(FULL, b, o);
+        }
+    }
+    return make_float2(a, b);
+}
+
+// A thread's columns of a row as they lie in memory, loaded ahead of their use.
+template <typename T, int VEC, int NV> struct LnRow { Pack<T, VEC> p[NV]; };
+template <typename T, int VEC, int NV, int TPR>
+__device__ __forceinline__ void ln_fetch(const T* row, int t, int width, LnRow<T, VEC, NV>& r) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int col = (i * TPR + t) * VEC;
+        if (col + VEC <= width) {
+            r.p[i] = *reinterpret_cast<const Pack<T, VEC>*>(row + col);
+        } else {
+            uint32_t b[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) b[j] = col + j < width ? bits_of<T>(Elem<T>::up(row[col + j])) : 0u;
+            if constexpr (sizeof(T) == 4 || VEC == 1) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) set_word(r.p[i], j, b[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; j += 2) set_word(r.p[i], j / 2, b[j] | (b[j + 1] << 16));
+            }
+        }
+    }
+}
+// a thread's columns of a vector of `width` parameters
+template <int VEC, int NV, int TPR>
+__device__ __forceinline__ void ln_params(const float* p, float other, int t, int width, float (&v)[NV][VEC]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int c = (i * TPR + t) * VEC + j;
+            v[i][j] = p && c < width ? __ldg(p + c) : other;
+        }
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void ln_store(T* p, int col, int width, const float (&v)[VEC]) {
+    if (VEC == 1 || col + VEC <= width) {
+        if (VEC > 1 || col < width) store_down<T, VEC>(p + col, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (col + j < width) p[col + j] = Elem<T>::down(v[j]);
+    }
+}
+
+// gamma and beta stay in registers over a thread's rows, and two more rows are on their way while this one is reduced.
+// WHOLE: the row fills the threads' columns exactly; its moments take one barrier and no comparisons of columns with the width.
+// The 16384 x 4096 bf16 case is as close to the issue rate as to HBM: with values converted three times, comparisons and
+// quotients in the joins it took 128 us.
+template <typename T, int VEC, int NV, int TPR, bool WHOLE>
+__global__ void __launch_bounds__(LN_THREADS, ln_blocks(3 * NV * VEC + 2 * NV * VEC * int(sizeof(T)) / 4 + 16)) layer_norm_kernel(const LnParams P) {
+    __shared__ float2 part[2][LN_THREADS / 32];
+    constexpr int RPB = LN_THREADS / TPR;
+    const int t = threadIdx.x % TPR;
+    const int64_t step = int64_t(gridDim.x) * RPB;
+    int64_t row = int64_t(blockIdx.x) * RPB + threadIdx.x / TPR;
+    const float inv = 1.0f / float(P.width);
+    const int width = WHOLE ? NV * TPR * VEC : P.width;
+    chain_launch();
+    chain_wait();
+    LnRow<T, VEC, NV> next, after;
+    auto fetch = [&](int64_t r, LnRow<T, VEC, NV>& to) {
+        if (r < P.rows) ln_fetch<T, VEC, NV, TPR>(static_cast<const T*>(P.x) + r * P.ldx, t, width, to);
+    };
+    fetch(row, next);
+    fetch(row + step, after);
+    float gamma[NV][VEC], beta[NV][VEC];
+    ln_params<VEC, NV, TPR>(P.gamma, 1.0f, t, width, gamma);
+    ln_params<VEC, NV, TPR>(P.beta, 0.0f, t, width, beta);
+    for (int turn = 0; row < P.rows; row += step, turn ^= 1) {
+        float v[NV][VEC], mean = 0.0f, m2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[i][j] = pack_get<T, VEC>(next.p[i], j);          // 0 beyond the row
+                mean += v[i][j];
+            }
+        next = after;
+        fetch(row + 2 * step, after);
+        if (WHOLE) {
+            mean *= 1.0f / float(NV * VEC);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) m2 += (v[i][j] - mean) * (v[i][j] - mean);
+            row_moments<TPR, NV * VEC>(mean, m2, part, turn);
+        } else {
+            mean = row_sum<TPR>(mean, &part[0][0].x) * inv;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float d = v[i][j] - mean;
+                    m2 += (i * TPR + t) * VEC + j < width ? d * d : 0.0f;
+                }
+            m2 = row_sum<TPR>(m2, &part[1][0].x);
+        }
+        const float rstd = rsqrtf(m2 * inv + P.eps);
+        T* y = static_cast<T*>(P.y) + row * P.ldy;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * TPR + t) * VEC;
+            if (col < width) {
+                float o[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o[j] = (v[i][j] - mean) * rstd * gamma[i][j] + beta[i][j];
+                ln_store<T, VEC>(y, col, width, o);
+            }
+        }
+        if (t == 0) {
+            if (P.mean) P.mean[row] = mean;
+            if (P.rstd) P.rstd[row] = rstd;
+        }
+    }
+}
+
+// Rows too long for registers: one pass forms mean and squared differences with Welford's update, the threads' triples
+// are merged pairwise, a second pass (of a row that is then in L2) writes y.
 template <typename T>
 __global__ void __launch_bounds__(LN_THREADS) layer_norm_wide_kernel(const LnParams P) {
     __shared__ LnMoments part[LN_THREADS / 32];
@@ -167,7 +239,7 @@ __global__ void __launch_bounds__(LN_THREADS) layer_norm_wide_kernel(const LnPar
         __syncthreads();
         m = part[0];
         for (int w = 1; w < LN_THREADS / 32; ++w) m = ln_merge(m, part[w]);
-        const float mean = m.mean, rstd = 1.0f / sqrtf(m.m2 / float(P.width) + P.eps);
+        const float mean = m.mean, rstd = rsqrtf(m.m2 / float(P.width) + P.eps);
         T* y = static_cast<T*>(P.y) + row * P.ldy;
         for (int c = threadIdx.x; c < P.width; c += LN_THREADS) {
             const float g = P.gamma ? P.gamma[c] : 1.0f, b = P.beta ? P.beta[c] : 0.0f;
@@ -183,47 +255,57 @@ __global__ void __launch_bounds__(LN_THREADS) layer_norm_wide_kernel(const LnPar
 // Backward. A block walks over rows with a fixed assignment of columns to threads, so each thread keeps its columns' sums for
 // dgamma and dbeta in registers; the blocks' sums go to scratch and a second kernel adds them in block order.
 template <typename T, int VEC, int NV, int TPR, bool DW>
-__global__ void __launch_bounds__(LN_THREADS) layer_norm_backward_kernel(const LnParams P) {
-    __shared__ float2 red[LN_THREADS / 32];
-    extern __shared__ float cols[];                       // TPR = 32: [2][width], to join the warps' sums
+__global__ void __launch_bounds__(LN_THREADS, ln_blocks(5 * NV * VEC + (NV * VEC <= 16 ? 4 : 2) * NV * VEC * int(sizeof(T)) / 4 + 24)) layer_norm_backward_kernel(const LnParams P) {
+    __shared__ float2 part[2][LN_THREADS / 32];
+    extern __shared__ float cols[];                       // TPR = 32: [warps][2][width], to join the warps' sums
     constexpr int RPB = LN_THREADS / TPR;
+    constexpr bool AHEAD = NV * VEC <= 16;                // room for the next row in registers
     const int t = threadIdx.x % TPR;
+    const int64_t step = int64_t(gridDim.x) * RPB;
+    int64_t row = int64_t(blockIdx.x) * RPB + threadIdx.x / TPR;
     const float inv = 1.0f / float(P.width);
-    float dg[NV][VEC], db[NV][VEC];
+    float dg[NV][VEC], db[NV][VEC], gamma[NV][VEC];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) dg[i][j] = db[i][j] = 0.0f;
     chain_launch();
     chain_wait();
-    for (int64_t row = int64_t(blockIdx.x) * RPB + threadIdx.x / TPR; row < P.rows; row += int64_t(gridDim.x) * RPB) {
-        const T* x = static_cast<const T*>(P.x) + row * P.ldx;
-        const T* dy = static_cast<const T*>(P.dy) + row * P.lddy;
-        float xh[NV][VEC], w[NV][VEC];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            ln_load<T, VEC>(x, (i * TPR + t) * VEC, P.width, xh[i]);
-            ln_load<T, VEC>(dy, (i * TPR + t) * VEC, P.width, w[i]);
+    if (AHEAD) ln_params<VEC, NV, TPR>(P.gamma, 1.0f, t, P.width, gamma);
+    LnRow<T, VEC, NV> x, dy, x2, dy2;
+    float mean = 0.0f, rstd = 0.0f, mean2 = 0.0f, rstd2 = 0.0f;
+    auto fetch = [&](int64_t r, LnRow<T, VEC, NV>& a, LnRow<T, VEC, NV>& b, float& mu, float& rs) {
+        if (r < P.rows) {
+            ln_fetch<T, VEC, NV, TPR>(static_cast<const T*>(P.x) + r * P.ldx, t, P.width, a);
+            ln_fetch<T, VEC, NV, TPR>(static_cast<const T*>(P.dy) + r * P.lddy, t, P.width, b);
+            mu = P.mean_in[r];
+            rs = P.rstd_in[r];
         }
-        const float mean = P.mean_in[row], rstd = P.rstd_in[row];
+    };
+    if (AHEAD) fetch(row, x, dy, mean, rstd);
+    for (int turn = 0; row < P.rows; row += step, turn ^= 1) {
+        if (AHEAD) fetch(row + step, x2, dy2, mean2, rstd2);
+        else fetch(row, x, dy, mean, rstd);
+        if (!AHEAD) ln_params<VEC, NV, TPR>(P.gamma, 1.0f, t, P.width, gamma);
+        float xh[NV][VEC], w[NV][VEC];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const int c = (i * TPR + t) * VEC + j;
-                const bool in = c < P.width;
-                xh[i][j] = in ? (xh[i][j] - mean) * rstd : 0.0f;
+                const bool in = VEC == 1 || (i * TPR + t) * VEC + j < P.width;
+                xh[i][j] = in ? (pack_get<T, VEC>(x.p[i], j) - mean) * rstd : 0.0f;
+                w[i][j] = pack_get<T, VEC>(dy.p[i], j);      // 0 beyond the row
                 if (DW) {
                     dg[i][j] += w[i][j] * xh[i][j];
                     db[i][j] += w[i][j];
                 }
-                if (P.gamma) w[i][j] *= in ? __ldg(P.gamma + c) : 0.0f;
+                w[i][j] *= gamma[i][j];
                 s1 += w[i][j];
                 s2 += w[i][j] * xh[i][j];
             }
         if (P.dx) {
-            const float2 s = row_sum2<TPR>(s1, s2, red);
+            const float2 s = row_sum2<TPR>(s1, s2, part, turn);
             const float m1 = s.x * inv, m2 = s.y * inv;
             T* dx = static_cast<T*>(P.dx) + row * P.lddx;
 #pragma unroll
@@ -237,37 +319,29 @@ __global__ void __launch_bounds__(LN_THREADS) layer_norm_backward_kernel(const L
                 }
             }
         }
+        if (AHEAD) { x = x2; dy = dy2; mean = mean2; rstd = rstd2; }
     }
     if (DW) {
         float* out = P.partial + int64_t(blockIdx.x) * 2 * P.width;
-        if (TPR == 32) {                                  // the warps in turn: a fixed order of additions
-            for (int wp = 0; wp < RPB; ++wp) {
-                if (int(warp_id()) == wp) {
+        float* to = TPR == 32 ? cols + warp_id() * 2 * P.width : out;
 #pragma unroll
-                    for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                        for (int j = 0; j < VEC; ++j) {
-                            const int c = (i * TPR + t) * VEC + j;
-                            if (c < P.width) {
-                                cols[c] = (wp ? cols[c] : 0.0f) + dg[i][j];
-                                cols[P.width + c] = (wp ? cols[P.width + c] : 0.0f) + db[i][j];
-                            }
-                        }
+            for (int j = 0; j < VEC; ++j) {
+                const int c = (i * TPR + t) * VEC + j;
+                if (c < P.width) {
+                    to[c] = dg[i][j];
+                    to[P.width + c] = db[i][j];
                 }
-                __syncthreads();
             }
-            for (int c = threadIdx.x; c < 2 * P.width; c += LN_THREADS) out[c] = cols[c];
-        } else {
+        if (TPR == 32) {                                  // the warps' sums, in their order
+            __syncthreads();
+            for (int c = threadIdx.x; c < 2 * P.width; c += LN_THREADS) {
+                float s = cols[c];
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int c = (i * TPR + t) * VEC + j;
-                    if (c < P.width) {
-                        out[c] = dg[i][j];
-                        out[P.width + c] = db[i][j];
-                    }
-                }
+                for (int wp = 1; wp < RPB; ++wp) s += cols[wp * 2 * P.width + c];
+                out[c] = s;
+            }
         }
     }
 }
@@ -275,10 +349,11 @@ __global__ void __launch_bounds__(LN_THREADS) layer_norm_backward_kernel(const L
 // Rows too long for registers: dx by two passes over the row, the columns' sums by a kernel of their own.
 template <typename T>
 __global__ void __launch_bounds__(LN_THREADS) layer_norm_backward_wide_kernel(const LnParams P) {
-    __shared__ float2 red[LN_THREADS / 32];
+    __shared__ float2 part[2][LN_THREADS / 32];
     chain_launch();
     chain_wait();
-    for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x) {
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x, turn ^= 1) {
         const T* x = static_cast<const T*>(P.x) + row * P.ldx;
         const T* dy = static_cast<const T*>(P.dy) + row * P.lddy;
         const float mean = P.mean_in[row], rstd = P.rstd_in[row];
@@ -288,7 +363,7 @@ __global__ void __launch_bounds__(LN_THREADS) layer_norm_backward_wide_kernel(co
             s1 += w;
             s2 += w * ((Elem<T>::up(x[c]) - mean) * rstd);
         }
-        const float2 s = row_sum2<LN_THREADS>(s1, s2, red);
+        const float2 s = row_sum2<LN_THREADS>(s1, s2, part, turn);
         const float m1 = s.x / float(P.width), m2 = s.y / float(P.width);
         T* dx = static_cast<T*>(P.dx) + row * P.lddx;
         for (int c = threadIdx.x; c < P.width; c += LN_THREADS) {

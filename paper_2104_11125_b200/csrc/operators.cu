@@ -103,11 +103,26 @@ cudaError_t launch(scalecom_ops* o, void (*kernel)(A...), dim3 grid, int threads
 int enter(scalecom_ops* o) { return !o ? SCALECOM_ERR_NULL_PTR : o->poisoned ? SCALECOM_ERR_BAD_STATE : SCALECOM_OK; }
 
 // ---- layer norm --------------------------------------------------------------------------------------------
-template <typename T, int VEC, int NV, int TPR>
-cudaError_t ln_launch(scalecom_ops* o, const LnParams& P) {
-    const int64_t want = ceil_div(P.rows, LN_THREADS / TPR), cap = int64_t(o->sms) * 8;
-    return launch(o, layer_norm_kernel<T, VEC, NV, TPR>, dim3(unsigned(want < cap ? want : cap)), LN_THREADS, 0, P);
+constexpr int LN_MOST_BLOCKS = 4;       // of a backward kernel on a multiprocessor: bounds the scratch
+
+// blocks of a kernel that fit the device at once
+template <typename K>
+int64_t resident(const scalecom_ops* o, K kernel, int threads, size_t smem, int most = 32) {
+    int per = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, threads, smem) != cudaSuccess || per < 1) per = 1;
+    if (per > most) per = most;
+    return int64_t(o->sms) * per;
 }
+
+template <typename T, int VEC, int NV, int TPR, bool WHOLE = false>
+cudaError_t ln_launch(scalecom_ops* o, const LnParams& P) {
+    if constexpr (!WHOLE && VEC > 1)
+        if (P.width == NV * VEC * TPR) return ln_launch<T, VEC, NV, TPR, true>(o, P);
+    static const int64_t cap = resident(o, layer_norm_kernel<T, VEC, NV, TPR, WHOLE>, LN_THREADS, 0);
+    const int64_t want = ceil_div(P.rows, LN_THREADS / TPR);
+    return launch(o, layer_norm_kernel<T, VEC, NV, TPR, WHOLE>, dim3(unsigned(want < cap ? want : cap)), LN_THREADS, 0, P);
+}
+// A warp takes a row of up to 32 elements a lane, without a barrier; wider rows take a block.
 template <typename T, int VEC>
 cudaError_t ln_forward(scalecom_ops* o, const LnParams& P) {
     const int w = P.width;
@@ -115,10 +130,12 @@ cudaError_t ln_forward(scalecom_ops* o, const LnParams& P) {
     if (w <= W) return ln_launch<T, VEC, 1, 32>(o, P);
     if (w <= 2 * W) return ln_launch<T, VEC, 2, 32>(o, P);
     if (w <= 4 * W) return ln_launch<T, VEC, 4, 32>(o, P);
+    if (VEC <= 4 && w <= 8 * W) return ln_launch<T, VEC, VEC <= 4 ? 8 : 1, 32>(o, P);
     if (w <= B) return ln_launch<T, VEC, 1, LN_THREADS>(o, P);
     if (w <= 2 * B) return ln_launch<T, VEC, 2, LN_THREADS>(o, P);
     if (w <= 4 * B) return ln_launch<T, VEC, 4, LN_THREADS>(o, P);
-    if (VEC == 1 && w <= 16 * B) return ln_launch<T, VEC, VEC == 1 ? 16 : 1, LN_THREADS>(o, P);
+    if (VEC <= 4 && w <= 8 * B) return ln_launch<T, VEC, VEC <= 4 ? 8 : 1, LN_THREADS>(o, P);
+    if (VEC == 1 && w <= 32 * B) return ln_launch<T, VEC, VEC == 1 ? 32 : 1, LN_THREADS>(o, P);
     const int64_t cap = int64_t(o->sms) * 8;
     return launch(o, layer_norm_wide_kernel<T>, dim3(unsigned(P.rows < cap ? P.rows : cap)), LN_THREADS, 0, P);
 }
@@ -129,15 +146,26 @@ cudaError_t ln_forward_t(scalecom_ops* o, const LnParams& P) {
     return vec ? ln_forward<T, V>(o, P) : ln_forward<T, 1>(o, P);
 }
 
-// the backward pass keeps two sums a column in registers, so its rows leave the registers earlier
+template <typename T, int VEC, int NV, int TPR, bool DW>
+cudaError_t ln_launch_backward_dw(scalecom_ops* o, LnParams& P) {
+    const auto kernel = layer_norm_backward_kernel<T, VEC, NV, TPR, DW>;
+    const size_t smem = DW && TPR == 32 ? size_t(P.width) * 8 * (LN_THREADS / 32) : 0;
+    constexpr size_t most = DW && TPR == 32 ? size_t(NV) * VEC * 32 * 8 * (LN_THREADS / 32) : 0;
+    static const cudaError_t set = most > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)) : cudaSuccess;
+    if (set != cudaSuccess) return set;
+    static const int64_t fit = resident(o, kernel, LN_THREADS, most, LN_MOST_BLOCKS);
+    int64_t blocks = ceil_div(P.rows, LN_THREADS / TPR);
+    if (blocks > fit) blocks = fit;
+    // each block leaves a partial sum that is written and read again: at most an eighth of the rows' own traffic
+    const int64_t few = P.rows * 3 * int64_t(sizeof(T)) / 128;
+    if (DW && blocks > few) blocks = few > o->sms ? few : blocks < o->sms ? blocks : o->sms;
+    P.nblocks = int32_t(blocks);
+    return launch(o, kernel, dim3(P.nblocks), LN_THREADS, smem, P);
+}
 template <typename T, int VEC, int NV, int TPR>
 cudaError_t ln_launch_backward(scalecom_ops* o, LnParams& P) {
-    const int64_t want = ceil_div(P.rows, LN_THREADS / TPR), cap = int64_t(o->sms) * 2;
-    P.nblocks = int32_t(want < cap ? want : cap);
-    const size_t smem = TPR == 32 ? size_t(P.width) * 8 : 0;
-    if (P.dgamma || P.dbeta)
-        return launch(o, layer_norm_backward_kernel<T, VEC, NV, TPR, true>, dim3(P.nblocks), LN_THREADS, smem, P);
-    return launch(o, layer_norm_backward_kernel<T, VEC, NV, TPR, false>, dim3(P.nblocks), LN_THREADS, 0, P);
+    if (P.dgamma || P.dbeta) return ln_launch_backward_dw<T, VEC, NV, TPR, true>(o, P);
+    return ln_launch_backward_dw<T, VEC, NV, TPR, false>(o, P);
 }
 template <typename T, int VEC>
 cudaError_t ln_backward(scalecom_ops* o, LnParams& P) {
@@ -146,16 +174,17 @@ cudaError_t ln_backward(scalecom_ops* o, LnParams& P) {
     if (w <= W) return ln_launch_backward<T, VEC, 1, 32>(o, P);
     if (w <= 2 * W) return ln_launch_backward<T, VEC, 2, 32>(o, P);
     if (w <= 4 * W) return ln_launch_backward<T, VEC, 4, 32>(o, P);
+    if (VEC <= 4 && w <= 8 * W) return ln_launch_backward<T, VEC, VEC <= 4 ? 8 : 1, 32>(o, P);
     if (w <= B) return ln_launch_backward<T, VEC, 1, LN_THREADS>(o, P);
     if (w <= 2 * B) return ln_launch_backward<T, VEC, 2, LN_THREADS>(o, P);
     if (w <= 4 * B) return ln_launch_backward<T, VEC, 4, LN_THREADS>(o, P);
     if (VEC <= 4 && w <= 8 * B) return ln_launch_backward<T, VEC, VEC <= 4 ? 8 : 1, LN_THREADS>(o, P);
-    if (VEC == 1 && w <= 16 * B) return ln_launch_backward<T, VEC, VEC == 1 ? 16 : 1, LN_THREADS>(o, P);
+    if (VEC == 1 && w <= 32 * B) return ln_launch_backward<T, VEC, VEC == 1 ? 32 : 1, LN_THREADS>(o, P);
     if (P.dgamma || P.dbeta) {                            // before dx, which may overwrite dy
         const int64_t cols = ceil_div(w, LN_THREADS);
         int64_t groups = ceil_div(int64_t(o->sms) * 8, cols);
         if (groups > P.rows) groups = P.rows;
-        if (groups > o->sms * 2) groups = o->sms * 2;
+        if (groups > o->sms * LN_MOST_BLOCKS) groups = o->sms * LN_MOST_BLOCKS;
         P.nblocks = int32_t(groups);
         const cudaError_t e = launch(o, layer_norm_columns_kernel<T>, dim3(unsigned(cols), unsigned(groups)), LN_THREADS, 0, P);
         if (e != cudaSuccess) return e;
@@ -857,7 +886,7 @@ int scalecom_layer_norm_backward(scalecom_ops* o, int32_t dtype, int64_t rows, i
     if (!dx && !dgamma && !dbeta) return SCALECOM_OK;
     const bool dw = dgamma || dbeta;
     if (dw) {
-        rc = ensure_ws(o, size_t(o->sms) * 2 * 2 * size_t(width) * 4);
+        rc = ensure_ws(o, size_t(o->sms) * LN_MOST_BLOCKS * 2 * size_t(width) * 4);
         if (rc != SCALECOM_OK) return rc;
     }
     LnParams P;

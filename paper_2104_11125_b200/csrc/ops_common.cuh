@@ -27,20 +27,60 @@ template <> struct Elem<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 down(float v) { return __float2bfloat16_rn(v); }
 };
 
-// N elements of T as one object that a single load or store moves (N * sizeof(T) <= 16)
-template <typename T, int N> struct alignas(N * sizeof(T)) Pack { T e[N]; };
+// N elements of T as the words that a single load or store moves (N * sizeof(T) <= 16). Built-in vector types on purpose: a struct
+// of 16-bit elements is copied element by element (measured: a bf16 layer norm at 1.5 TB/s).
+template <int BYTES> struct Words;
+template <> struct Words<16> { typedef uint4 type; };
+template <> struct Words<8> { typedef uint2 type; };
+template <> struct Words<4> { typedef uint32_t type; };
+template <> struct Words<2> { typedef uint16_t type; };
+template <typename T, int N> using Pack = typename Words<N * sizeof(T)>::type;
 
+__device__ __forceinline__ uint32_t word_of(const uint4& p, int i) { return i == 0 ? p.x : i == 1 ? p.y : i == 2 ? p.z : p.w; }
+__device__ __forceinline__ uint32_t word_of(const uint2& p, int i) { return i == 0 ? p.x : p.y; }
+__device__ __forceinline__ uint32_t word_of(const uint32_t& p, int) { return p; }
+__device__ __forceinline__ uint32_t word_of(const uint16_t& p, int) { return p; }
+__device__ __forceinline__ void set_word(uint4& p, int i, uint32_t v) { (i == 0 ? p.x : i == 1 ? p.y : i == 2 ? p.z : p.w) = v; }
+__device__ __forceinline__ void set_word(uint2& p, int i, uint32_t v) { (i == 0 ? p.x : p.y) = v; }
+__device__ __forceinline__ void set_word(uint32_t& p, int, uint32_t v) { p = v; }
+__device__ __forceinline__ void set_word(uint16_t& p, int, uint32_t v) { p = uint16_t(v); }
+
+// element i of a pack (i a constant after unrolling)
+template <typename T, int N> __device__ __forceinline__ float pack_get(const Pack<T, N>& p, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(word_of(p, i));
+    const uint32_t w = word_of(p, i / 2);
+    if constexpr (Elem<T>::id == SCALECOM_BF16) return __uint_as_float((i & 1) ? w & 0xFFFF0000u : w << 16);
+    return __half2float(__ushort_as_half(uint16_t((i & 1) ? w >> 16 : w & 0xFFFFu)));
+}
+template <typename T> __device__ __forceinline__ uint32_t bits_of(float v) {
+    if constexpr (Elem<T>::id == SCALECOM_F32) return __float_as_uint(v);
+    else if constexpr (Elem<T>::id == SCALECOM_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    else return __half_as_ushort(__float2half_rn(v));
+}
 template <typename T, int N>
 __device__ __forceinline__ void load_up(const T* p, float (&v)[N]) {
     const Pack<T, N> t = *reinterpret_cast<const Pack<T, N>*>(p);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = Elem<T>::up(t.e[i]);
+    for (int i = 0; i < N; ++i) v[i] = pack_get<T, N>(t, i);
 }
 template <typename T, int N>
 __device__ __forceinline__ void store_down(T* p, const float (&v)[N]) {
     Pack<T, N> t;
+    if constexpr (sizeof(T) == 4 || N == 1) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) t.e[i] = Elem<T>::down(v[i]);
+        for (int i = 0; i < N; ++i) set_word(t, i, bits_of<T>(v[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            if constexpr (Elem<T>::id == SCALECOM_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[i], v[i + 1]);
+                set_word(t, i / 2, *reinterpret_cast<const uint32_t*>(&h));
+            } else {
+                const __half2 h = __floats2half2_rn(v[i], v[i + 1]);
+                set_word(t, i / 2, *reinterpret_cast<const uint32_t*>(&h));
+            }
+        }
+    }
     *reinterpret_cast<Pack<T, N>*>(p) = t;
 }
 
