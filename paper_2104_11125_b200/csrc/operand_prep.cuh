@@ -75,6 +75,9 @@ __global__ void __launch_bounds__(PREP_THREADS) prep_amax_kernel(const __grid_co
     const PrepItem& I = T.item[blockIdx.y];
     const int64_t groups = (I.cols + 7) / 8;
     const int tx = prep_tx(groups), ty = PREP_THREADS / tx;
+    __shared__ uint32_t block_top;
+    if (threadIdx.x == 0) block_top = 0u;
+    __syncthreads();
     uint32_t top = 0u;
     for (int64_t r = int64_t(blockIdx.x) * ty + threadIdx.x / tx; r < I.rows; r += int64_t(gridDim.x) * ty)
         for (int64_t g = threadIdx.x % tx; g < groups; g += tx) {
@@ -84,7 +87,10 @@ __global__ void __launch_bounds__(PREP_THREADS) prep_amax_kernel(const __grid_co
             for (int i = 0; i < 8; ++i) top = max(top, finite_bits(v[i]));
         }
     top = __reduce_max_sync(FULL, top);
-    if (lane_id() == 0 && top) atomicMax(I.amax, top);    // a maximum: the order does not matter
+    if (lane_id() == 0) atomicMax(&block_top, top);
+    __syncthreads();
+    // a maximum: the order does not matter. One word takes an atomic a nanosecond, so only those that raise it are sent.
+    if (threadIdx.x == 0 && block_top > ld_relaxed_u32(I.amax)) atomicMax(I.amax, block_top);
 }
 
 __global__ void __launch_bounds__(PREP_THREADS) prep_operand_kernel(const __grid_constant__ PrepTable T) {

@@ -11,6 +11,7 @@
 #include <utility>
 
 #include "layer_norm.cuh"
+#include "ns_small.cuh"
 #include "operand_prep.cuh"
 #include "ops_common.cuh"
 #include "tc_product.cuh"
@@ -619,11 +620,65 @@ struct NsArgs {
     float eps, scale;
 };
 
+// Blocks of a cluster for the one-launch kernel, 0: the separate products are taken. By the least estimated cycles: a product of
+// 16 x 8 x 16 takes 20 on a quarter of an SM, a cluster's barriers and sums some thousands a step; the chain of separate products measured
+// 110 us for small matrices (180 with two planes) and then runs at about half the tensor cores' rate on tiles of 256 rows.
+int small_cluster(const scalecom_ops* o, int planes, int64_t r, int64_t n, int64_t batch, int steps) {
+    if (r > NSS_MAX_R) return 0;
+    const int64_t rp = (r + 15) / 16 * 16, side = rp / 16, tiles = side * (side + 1) / 2;
+    const double chain = steps / 5.0 * ((planes > 1 ? 330e3 : 200e3) + double(batch) * n * 256.0 * 256.0 * 15.0 * (planes > 1 ? 3 : 1) / (o->sms * 4096.0));
+    double least = chain;
+    int best = 0;
+    for (int c = 1; c <= 8; c *= 2) {
+        const int64_t nc = (ceil_div(n, c) + 15) / 16 * 16;
+        if (nss_smem(planes, rp, nc, c) > 225 * 1024) continue;
+        const double waves = double(ceil_div(batch * c, o->sms));
+        const double mma = 2.0 * (tiles * (nc / 16) + tiles * side + (nc / 16) * side * side) * (planes > 1 ? 3 : 1);
+        const double cost = waves * (steps * (mma * 20.0 / 4.0 + 1500.0 + (c > 1 ? 7000.0 + 1500.0 * ceil_div(tiles, NSS_WARPS) * ceil_div(c, 4) : 0.0)) + 4000.0 + double(rp) * nc / 16.0);
+        if (cost < least * 0.95) {
+            least = cost;
+            best = c;
+        }
+    }
+    return best;
+}
+template <int PL>
+cudaError_t small_attribute() {
+    const cudaError_t e = cudaFuncSetAttribute(ns_small_kernel<PL, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(ns_small_kernel<PL, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
+}
+int orthogonalise_small(scalecom_ops* o, const NsArgs& A, int planes, int cluster) {
+    NsSmallParams P;
+    std::memset(&P, 0, sizeof P);
+    P.tall = A.rows > A.cols;
+    P.in = A.in; P.out = A.out;
+    P.ld_in = A.ld_in; P.in_stride = A.in_stride; P.ld_out = A.ld_out; P.out_stride = A.out_stride;
+    P.in_type = A.in_type; P.out_type = A.out_type;
+    P.r = int32_t(P.tall ? A.cols : A.rows);
+    P.n = int32_t(P.tall ? A.rows : A.cols);
+    P.rp = (P.r + 15) / 16 * 16;
+    P.nc = int32_t((ceil_div(P.n, cluster) + 15) / 16 * 16);
+    P.steps = A.steps; P.ncoef = A.ncoef; P.eps = A.eps; P.scale = A.scale;
+    for (int i = 0; i < 3 * A.ncoef; ++i) P.co[i] = A.co[i];
+    const size_t smem = size_t(nss_smem(planes, P.rp, P.nc, cluster));
+    const dim3 grid{unsigned(cluster), unsigned(A.batch)};
+    auto go = [&](auto kernel) { return launch_cluster(o, cluster, kernel, grid, NSS_THREADS, smem, P); };
+    const cudaError_t e = planes > 1 ? (cluster > 1 ? go(ns_small_kernel<2, true>) : go(ns_small_kernel<2, false>))
+                                     : (cluster > 1 ? go(ns_small_kernel<1, true>) : go(ns_small_kernel<1, false>));
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return SCALECOM_ERR_CUDA;
+    }
+    return SCALECOM_OK;
+}
+
 int orthogonalise(scalecom_ops* o, const NsArgs& A) {
     const int planes = A.out_type == SCALECOM_F32 ? 2 : 1;
     const bool tall = A.rows > A.cols;
     const int64_t r = tall ? A.cols : A.rows, big = tall ? A.rows : A.cols;
     const int64_t ldx = pad8(A.cols), lda = pad8(r), B = A.batch;
+    const int cluster = A.steps ? small_cluster(o, planes, r, big, B, A.steps) : 0;
+    if (cluster) return orthogonalise_small(o, A, planes, cluster);
     int64_t nparts = ceil_div(A.rows * A.cols, 1 << 14);
     if (nparts > ceil_div(int64_t(o->sms) * 4, B)) nparts = ceil_div(int64_t(o->sms) * 4, B);
     if (nparts > A.rows) nparts = A.rows;
@@ -763,6 +818,8 @@ int scalecom_ops_create(scalecom_ops** out) {
     if (e == cudaSuccess) e = tc_attributes<EPI_GRAM>();
     if (e == cudaSuccess) e = tc_attributes<EPI_POLY>();
     if (e == cudaSuccess) e = tc_attributes<EPI_PLANES>();
+    if (e == cudaSuccess) e = small_attribute<1>();
+    if (e == cudaSuccess) e = small_attribute<2>();
     if (e != cudaSuccess) {
         cudaGetLastError();
         delete o;

@@ -21,7 +21,8 @@
 // PL = 2, for fp32 values: each operand is two fp16 planes, x = hi + lo, and a block of k contributes lo hi + hi lo + hi hi.
 // The tensor core truncates its fp32 accumulator after every 16 k (measured: 2.2e-8 of the result for each, always towards
 // zero, so 2048 k are 3e-6 low), which is why the accumulator is not kept there: after each 64 k, small products first, the epilogue
-// warps add it to sums in registers with correct rounding.
+// warps add it to sums in registers with correct rounding.  Three accumulators in turn cover the way from the tensor core to those warps
+// and back; the finished sums go to the fourth quarter of TMEM, from where the epilogue proceeds as with one plane.
 #pragma once
 #include <cuda.h>
 
@@ -36,7 +37,11 @@ constexpr int TC_EPI_WARPS = 8;
 constexpr int TC_EPI_THREADS = TC_EPI_WARPS * 32;
 constexpr int TC_A_BYTES = TC_BM * TC_BK * 2;
 
-constexpr int TC_RING = 8192;         // staging area of an epilogue warp: four 32 x 32 blocks of 16 bits, or two of 32
+// Staging area of an epilogue warp: two 32 x 32 blocks of 16 bits, or one of 32. What it takes, the operands in flight lack: from a
+// stage's last product to its next data being there takes some 2,800 cycles, so the products run at their rate only with
+// about 190 KB on their way (measured with 8 KB here: five stages of 32 KB, 620 cycles for 64 k that take 512).
+constexpr int TC_RING = 4096;
+constexpr int TC_CHUNK = 1;             // PL = 2: blocks of 64 k between two additions to the sums (two: a fifth faster, and errors of 1e-6 instead of 3.5e-7)
 
 template <int BN, int EPI, int PL, int CG> struct TcShape {
     static constexpr int B_BYTES = BN / CG * TC_BK * 2;
@@ -47,7 +52,8 @@ template <int BN, int EPI, int PL, int CG> struct TcShape {
     static constexpr int STAGES = (227 * 1024 - 1024 - 512 - EPI_BYTES) / STAGE_BYTES;
     static constexpr int BM = TC_BM * CG;                            // rows of a tile
     static constexpr int SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 1024;         // + alignment of the swizzle atoms
-    static constexpr int TMEM_COLS = 2 * BN;
+    static constexpr int ACCS = PL == 2 ? 3 : 2;                     // accumulators in TMEM
+    static constexpr int TMEM_COLS = PL == 2 ? 4 * BN : 2 * BN;      // PL = 2: and the sums
 };
 
 enum TcEpilogue { EPI_STORE = 0, EPI_GATE = 1, EPI_GATE_BWD = 2, EPI_GRAM = 3, EPI_POLY = 4, EPI_PLANES = 5 };
@@ -219,6 +225,22 @@ __device__ __forceinline__ uint32_t lds32(uint32_t at) {
     return v;
 }
 
+__device__ __forceinline__ void tc_st32(uint32_t addr, const float (&v)[32]) {
+    uint32_t r[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(v[i]);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+          "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+          "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // Shared-memory matrix descriptors, 128-byte swizzle (layout code 2, version 1).
 //   K-major:  a tile is rows of 128 bytes; 8 rows form an atom, atoms 1024 bytes apart.
 //   MN-major: a tile is 64-row-wide panels; in a panel each k is a 128-byte row, 8 k form an atom (1024 bytes
@@ -229,22 +251,22 @@ __device__ __forceinline__ uint64_t tc_desc(uint32_t addr, int mn) {
 }
 
 // ---- activations --------------------------------------------------------------------------------------
-// EXACT: CUDA's accurate exp and division, for fp32 results; else the fast ones (about 2^-21 relative), far below a 16-bit rounding.
-template <bool EXACT> __device__ __forceinline__ float act_sigmoid(float g) {
-    return EXACT ? 1.0f / (1.0f + expf(-g)) : __fdividef(1.0f, 1.0f + __expf(-g));
-}
+// The fast exp and division: 2 + 1.2 |x| units in the last place of fp32 for exp(x), 2 for the quotient, so a sigmoid is within a few
+// units in the last place wherever it is not negligible beside 1 -- below what the products before it lose, and a quarter
+// of the accurate functions' instructions, which set the pace of the backward epilogue.
+__device__ __forceinline__ float act_sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
 // value and derivative
-template <int ACT, bool EXACT>
+template <int ACT>
 __device__ __forceinline__ void act_both(float g, float& a, float& s) {
     if (ACT == SCALECOM_ACT_SILU) {
         // the fast division gives 0 for denominators beyond 2^126, which is the limit here
-        const float p = act_sigmoid<EXACT>(g);
+        const float p = act_sigmoid(g);
         a = g * p;
         s = p * (1.0f + g * (1.0f - p));
     } else if (ACT == SCALECOM_ACT_GELU) {
         const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
         a = g * c;
-        s = c + g * (EXACT ? expf(-0.5f * g * g) : __expf(-0.5f * g * g)) * 0.39894228040143268f;
+        s = c + g * __expf(-0.5f * g * g) * 0.39894228040143268f;
     } else if (ACT == SCALECOM_ACT_GELU_TANH) {
         if (fabsf(g) > 30.0f) {                 // tanh is +-1 there; the cube below could overflow
             a = g > 0.0f ? g : 0.0f;
@@ -260,21 +282,21 @@ __device__ __forceinline__ void act_both(float g, float& a, float& s) {
     }
 }
 // 32 columns at once, so that the choice of the activation is made once and not for each element
-template <int ACT, bool EXACT>
+template <int ACT>
 __device__ __forceinline__ void gate_row(const float (&g)[32], float (&v)[32], const float (&w)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
         float a, s;
-        act_both<ACT, EXACT>(g[i], a, s);
+        act_both<ACT>(g[i], a, s);
         v[i] = a * w[i];
     }
 }
-template <int ACT, bool EXACT>
+template <int ACT>
 __device__ __forceinline__ void gate_back_row(float (&g)[32], float (&v)[32], float (&w)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
         float a, s;
-        act_both<ACT, EXACT>(g[i], a, s);
+        act_both<ACT>(g[i], a, s);
         const float dh = v[i], u = w[i];
         g[i] = dh * u * s;             // dg
         w[i] = dh * a;                 // du
@@ -335,7 +357,7 @@ __device__ __forceinline__ uint32_t piece32(uint32_t row, uint32_t piece) { retu
 // the next free block of the ring; at most its own size in blocks are still being read by the stores issued before
 template <int BYTES>
 __device__ __forceinline__ uint32_t ring_next(Ring& r) {
-    constexpr int SLOTS = BYTES == 2 ? 4 : 2;
+    constexpr int SLOTS = BYTES == 2 ? 2 : 1;
     if (lane_id() == 0) bulk_wait_read<SLOTS - 1>();
     __syncwarp();
     return r.base + uint32_t(r.n++ & (SLOTS - 1)) * (TC_RING / SLOTS);
@@ -453,6 +475,20 @@ __device__ __forceinline__ void load_typed(int type, const void* base, int64_t o
     else load_row32(static_cast<const float*>(base) + off, v, ncols);
 }
 
+// Largest finite magnitude (bits) of a row's first nc columns. What lies beyond them are zeros (the operands' edges are filled with
+// zeros, and every epilogue maps zeros to zeros), so they need no test.
+__device__ __forceinline__ uint32_t row_top(const float (&v)[32], int nc) {
+    if (nc <= 0) return 0u;
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = fmaxf(m, fabsf(v[i]));       // NaN is passed over
+    if (m < INFINITY) return __float_as_uint(m);
+    uint32_t t = 0u;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t = max(t, finite_bits(v[i]));
+    return t;
+}
+
 // Blocks that an epilogue reads (GATE_BWD: g and u, POLY: A), one ahead of the block being worked on.
 struct Inflow {
     uint32_t smem, bar;
@@ -476,7 +512,7 @@ __device__ __forceinline__ void inflow_start(const TcParams& P, Inflow& f, int r
 
 // ---- epilogues on a block of 32 x 32: v (and w) hold this lane's row --------------------------------------------
 template <int EPI, int PL>
-__device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, int row0, int col0, float (&v)[32], float (&w)[32], float un,
+__device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, int row0, int col0, int col_next, float (&v)[32], float (&w)[32], float un,
                                             uint32_t& top, uint32_t& top2, Ring& ring, Inflow& in, volatile uint32_t* abort) {
     if (!block_used<EPI>(P, row0, col0)) return true;
     const int row = row0 + int(lane_id()), nc = P.n - col0;
@@ -492,14 +528,10 @@ __device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, 
             emit<PL == 2>(P, 1, ring, P.type, v, row0, col0, 0, 0);
             emit<PL == 2>(P, 1, ring, P.type, w, row0, col0, 1, 0);
         }
-#define SC_CALL(ACT) gate_row<ACT, PL == 2>(v, v, w)
+#define SC_CALL(ACT) gate_row<ACT>(v, v, w)
         SC_FOR_ACT(P.act, SC_CALL)
 #undef SC_CALL
-        if (PL == 2 && inside) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < nc) top = max(top, finite_bits(v[i]));
-        }
+        if (PL == 2) top = max(top, row_top(v, inside ? nc : 0));
         emit<PL == 2>(P, 0, ring, P.type, v, row0, col0, 0, 0);
     } else if (EPI == EPI_GATE_BWD) {
         float g[32];
@@ -510,6 +542,7 @@ __device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, 
             take16(in.smem, P.type, g);
             take16(in.smem + 2048u, P.type, w);
             __syncwarp();
+            if (col_next >= 0) inflow_start<EPI>(P, in, row0, col_next, u.batch);
         } else {
             const int64_t at = int64_t(row) * P.in_ld + col0;
             load_typed(P.type, P.in, at, g, inside ? nc : 0);
@@ -517,16 +550,12 @@ __device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, 
         }
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= un;
-#define SC_CALL(ACT) gate_back_row<ACT, PL == 2>(g, v, w)
+#define SC_CALL(ACT) gate_back_row<ACT>(g, v, w)
         SC_FOR_ACT(P.act, SC_CALL)
 #undef SC_CALL
-        if (PL == 2 && inside) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < nc) {
-                    top = max(top, max(finite_bits(g[i]), finite_bits(w[i])));
-                    top2 = max(top2, finite_bits(v[i]));
-                }
+        if (PL == 2) {
+            top = max(top, max(row_top(g, inside ? nc : 0), row_top(w, inside ? nc : 0)));
+            top2 = max(top2, row_top(v, inside ? nc : 0));
         }
         emit<PL == 2>(P, 0, ring, P.type, g, row0, col0, 0, 0);
         emit<PL == 2>(P, 0, ring, P.type, w, row0, col0, 1, 0);
@@ -544,6 +573,7 @@ __device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, 
                 in.pending = false;
                 take16(in.smem, SCALECOM_F16, w);
                 __syncwarp();
+                if (col_next >= 0) inflow_start<EPI>(P, in, row0, col_next, u.batch);
             } else {
                 const int64_t at = int64_t(u.batch) * P.in_batch + int64_t(row) * P.in_ld + col0;
                 load_typed(SCALECOM_F16, P.in, at, w, inside ? nc : 0);
@@ -575,7 +605,7 @@ template <int BN, int EPI, int PL, int CG>
 __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_constant__ TcParams P) {
     using S = TcShape<BN, EPI, PL, CG>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t bars[2 * S::STAGES + 4 + 1 + TC_EPI_WARPS];
+    __shared__ alignas(8) uint64_t bars[2 * S::STAGES + 2 * S::ACCS + 1 + TC_EPI_WARPS];
     __shared__ uint32_t tmem_base, abort_flag, last_flag;
 
     const uint32_t warp = warp_id(), lane = lane_id();
@@ -584,13 +614,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
     auto full = [&](int s) { return bar0 + 8u * s; };
     auto empty = [&](int s) { return bar0 + 8u * (S::STAGES + s); };
     auto tfull = [&](int s) { return bar0 + 8u * (2 * S::STAGES + s); };
-    auto tempty = [&](int s) { return bar0 + 8u * (2 * S::STAGES + 2 + s); };
-    const uint32_t drain = bar0 + 8u * (2 * S::STAGES + 4);
+    auto tempty = [&](int s) { return bar0 + 8u * (2 * S::STAGES + S::ACCS + s); };
+    const uint32_t drain = bar0 + 8u * (2 * S::STAGES + 2 * S::ACCS);
     const uint32_t inflow0 = drain + 8u;
 
     if (warp == 0 && lane == 0) {
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(tfull(s), 1); mbar_init(tempty(s), TC_EPI_WARPS * CG); }
+        for (int s = 0; s < S::ACCS; ++s) { mbar_init(tfull(s), 1); mbar_init(tempty(s), TC_EPI_WARPS * CG); }
         mbar_init(drain, 1);
         for (int w = 0; w < TC_EPI_WARPS; ++w) mbar_init(inflow0 + 8u * w, 1);
         abort_flag = 0u;
@@ -664,23 +694,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            int n_used = 0, n_acc = 0;
+            int n_used = 0, n_acc = 0;              // stages used, accumulators begun
             bool ok = true;
-            for (int un = first; ok && un < units; un += stride, ++n_acc) {
+            for (int un = first; ok && un < units; un += stride) {
                 const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
                 const int it0 = int(int64_t(iters) * u.split / P.splits), it1 = int(int64_t(iters) * (u.split + 1) / P.splits);
                 if (PL == 1) {
-                    if (!mbar_wait(tempty(n_acc & 1), ((n_acc >> 1) & 1) ^ 1, abort, P.status)) { ok = false; break; }
+                    if (!mbar_wait(tempty(n_acc % S::ACCS), ((n_acc / S::ACCS) & 1) ^ 1, abort, P.status)) { ok = false; break; }
                     tc_fence_after();
                 }
                 for (int it = it0; it < it1; ++it, ++n_used) {
                     const int s = n_used % S::STAGES;
-                    if (PL == 2) {                  // an accumulator for each block of k
-                        if (!mbar_wait(tempty(n_used & 1), ((n_used >> 1) & 1) ^ 1, abort, P.status)) { ok = false; break; }
-                    }
+                    const bool opens = PL == 2 && (it - it0) % TC_CHUNK == 0, closes = PL == 2 && ((it - it0) % TC_CHUNK == TC_CHUNK - 1 || it + 1 == it1);
+                    if (opens && !mbar_wait(tempty(n_acc % S::ACCS), ((n_acc / S::ACCS) & 1) ^ 1, abort, P.status)) { ok = false; break; }
                     if (!mbar_wait(full(s), (n_used / S::STAGES) & 1, abort, P.status)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t d = tmem + ((PL == 2 ? n_used : n_acc) & 1) * BN;
+                    const uint32_t d = tmem + (n_acc % S::ACCS) * BN;
                     const uint32_t a = tiles0 + s * S::STAGE_BYTES, b = a + PL * TC_A_BYTES;
                     const uint32_t step_a = P.a_mn ? 2048 >> 4 : 32 >> 4, step_b = P.b_mn ? 2048 >> 4 : 32 >> 4;
 #pragma unroll
@@ -689,12 +718,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                         const uint64_t db = tc_desc(b + (PL == 2 && t == 1 ? S::B_BYTES : 0), P.b_mn);
 #pragma unroll
                         for (int k = 0; k < TC_BK / 16; ++k)
-                            tc_mma<CG>(d, da + k * step_a, db + k * step_b, P.idesc, (t > 0 || k > 0 || (PL == 1 && it > it0)) ? 1u : 0u);
+                            tc_mma<CG>(d, da + k * step_a, db + k * step_b, P.idesc, (t > 0 || k > 0 || (PL == 2 ? !opens : it > it0)) ? 1u : 0u);
                     }
                     tc_commit<CG>(empty(s));
-                    if (PL == 2) tc_commit<CG>(tfull(n_used & 1));
+                    if (closes) tc_commit<CG>(tfull(n_acc++ % S::ACCS));
                 }
-                if (PL == 1 && ok) tc_commit<CG>(tfull(n_acc & 1));
+                if (PL == 1 && ok) tc_commit<CG>(tfull(n_acc++ % S::ACCS));
             }
             if (!ok) {                              // products in flight read shared memory and write TMEM
                 tc_commit<CG>(drain);
@@ -741,9 +770,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 for (int c = 0; c < BN / 64; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sum[c][i] = 0.0f;
-                for (int it = it0; it < it1; ++it, ++n_acc) {
-                    q = n_acc & 1;
-                    ok = __all_sync(FULL, mbar_wait(tfull(q), (n_acc >> 1) & 1, abort, P.status));
+                for (int it = it0; it < it1; it += TC_CHUNK, ++n_acc) {
+                    q = n_acc % S::ACCS;
+                    ok = __all_sync(FULL, mbar_wait(tfull(q), (n_acc / S::ACCS) & 1, abort, P.status));
                     if (!ok) break;
                     tc_fence_after();
                     acc = tmem + q * BN + lanes;
@@ -757,9 +786,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     __syncwarp();
                     if (lane == 0) acc_free(q);
                 }
+                acc = tmem + S::ACCS * BN + lanes;
+#pragma unroll
+                for (int c = 0; c < BN / 64; ++c) tc_st32(acc + column(c), sum[c]);
+                tc_wait_st();
             } else {
-                q = n_acc & 1;
-                ok = __all_sync(FULL, mbar_wait(tfull(q), (n_acc >> 1) & 1, abort, P.status));
+                q = n_acc % S::ACCS;
+                ok = __all_sync(FULL, mbar_wait(tfull(q), (n_acc / S::ACCS) & 1, abort, P.status));
                 ++n_acc;
                 acc = tmem + q * BN + lanes;
             }
@@ -778,18 +811,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 const int slot = u.tile * CG + int(rank);
                 float* mine = P.partial + (int64_t(slot) * P.splits) * (TC_BM * BN) + quad * 32 + lane;
                 float* put = mine + int64_t(u.split) * (TC_BM * BN);
-                if (PL == 2) {
-#pragma unroll
-                    for (int c = 0; c < BN / 64; ++c)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) put[(column(c) + i) * TC_BM] = sum[c][i];
-                } else {
 #pragma unroll 1
-                    for (int c = 0; c < BN / 64; ++c) {
-                        tc_ld32(acc + column(c), v);
+                for (int c = 0; c < BN / 64; ++c) {
+                    tc_ld32(acc + column(c), v);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) put[(column(c) + i) * TC_BM] = v[i];
-                    }
+                    for (int i = 0; i < 32; ++i) put[(column(c) + i) * TC_BM] = v[i];
                 }
                 release();
                 __threadfence();
@@ -820,13 +846,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     gather(at, v);
                     if (EPI == EPI_GATE) gather(BN / 2 + at, w);
                     begin(u, row0, c);
-                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, v, w, un_scale, top, top2, ring, in, abort);
-                }
-            } else if (PL == 2) {
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) {
-                    if (EPI == EPI_GATE) tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + chunk(c), sum[2 * c], sum[2 * c + 1], un_scale, top, top2, ring, in, abort);
-                    else tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + chunk(c), sum[c], w, un_scale, top, top2, ring, in, abort);
+                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, -1, v, w, un_scale, top, top2, ring, in, abort);
                 }
             } else {
 #pragma unroll 1
@@ -836,8 +856,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     if (EPI == EPI_GATE) tc_ld32(acc + BN / 2 + at, w);
                     if (c == CHUNKS - 1) release();
                     if (ok) begin(u, row0, c);
-                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, v, w, un_scale, top, top2, ring, in, abort);
-                    if (ok) begin(u, row0, c + 1);
+                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, c + 1 < CHUNKS ? u.nt * WIDTH + chunk(c + 1) : -1, v, w, un_scale,
+                                                    top, top2, ring, in, abort);
                 }
             }
         }
