@@ -14,7 +14,7 @@ STAMP = LIB + ".srchash"
 
 SOURCES = ["scalecom.cu", "topk_static.cu", "operators.cu"]
 HEADERS = ["common.cuh", "topk_select.cuh", "learner_pass.cuh", "chunk_select.cuh", "diagnostics.cuh", "exchange.cuh", "layer_topk.cuh", "small_step.cuh",
-           "ops_common.cuh", "layer_norm.cuh", "ns_small.cuh", "operand_prep.cuh", "tc_product.cuh"]
+           "ops_common.cuh", "ffn_tokens.cuh", "layer_norm.cuh", "ns_small.cuh", "operand_prep.cuh", "tc_product.cuh"]
 API_HEADERS = ["scalecom.h", "scalecom_operators.h"]
 
 NVCC_FLAGS = [

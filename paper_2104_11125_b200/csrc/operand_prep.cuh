@@ -31,7 +31,7 @@ __device__ __forceinline__ int prep_tx(int64_t groups) {
 }
 
 template <typename T>
-__device__ __forceinline__ void prep_load8(const T* p, int64_t left, float (&v)[8]) {
+__device__ __forceinline__ void prep_load8(const T* p, int64_t left, float (&v)[8], bool inside) {
     constexpr int N = 16 / sizeof(T) > 8 ? 8 : 16 / sizeof(T);
     if (left >= 8 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
 #pragma unroll
@@ -41,15 +41,29 @@ __device__ __forceinline__ void prep_load8(const T* p, int64_t left, float (&v)[
 #pragma unroll
             for (int j = 0; j < N; ++j) v[i + j] = t[j];
         }
+    } else if (sizeof(T) == 2 && left > 8 && inside) {
+        // off the grid, with neighbours of the same row on both sides: whole words, shifted by an element where they have to be
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(3));
+        const bool odd = (reinterpret_cast<uintptr_t>(p) & 2u) != 0;
+        uint32_t q[5];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = w[i];
+        q[4] = odd ? w[4] : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t t = odd ? __funnelshift_r(q[i], q[i + 1], 16) : q[i];
+            v[2 * i] = pack_get<T, 16 / sizeof(T)>(make_uint4(t, t, t, t), 0);
+            v[2 * i + 1] = pack_get<T, 16 / sizeof(T)>(make_uint4(t, t, t, t), 1);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < left ? Elem<T>::up(p[i]) : 0.0f;
     }
 }
-__device__ __forceinline__ void prep_load8_typed(int type, const void* base, int64_t off, int64_t left, float (&v)[8]) {
-    if (type == SCALECOM_F32) prep_load8(static_cast<const float*>(base) + off, left, v);
-    else if (type == SCALECOM_F16) prep_load8(static_cast<const __half*>(base) + off, left, v);
-    else prep_load8(static_cast<const __nv_bfloat16*>(base) + off, left, v);
+__device__ __forceinline__ void prep_load8_typed(int type, const void* base, int64_t off, int64_t left, float (&v)[8], bool inside) {
+    if (type == SCALECOM_F32) prep_load8(static_cast<const float*>(base) + off, left, v, inside);
+    else if (type == SCALECOM_F16) prep_load8(static_cast<const __half*>(base) + off, left, v, inside);
+    else prep_load8(static_cast<const __nv_bfloat16*>(base) + off, left, v, inside);
 }
 template <typename T>
 __device__ __forceinline__ void prep_store8(T* p, int64_t left, const float (&v)[8]) {
@@ -82,7 +96,7 @@ __global__ void __launch_bounds__(PREP_THREADS) prep_amax_kernel(const __grid_co
     for (int64_t r = int64_t(blockIdx.x) * ty + threadIdx.x / tx; r < I.rows; r += int64_t(gridDim.x) * ty)
         for (int64_t g = threadIdx.x % tx; g < groups; g += tx) {
             float v[8];
-            prep_load8(static_cast<const float*>(I.src) + r * I.ld + g * 8, I.cols - g * 8, v);
+            prep_load8(static_cast<const float*>(I.src) + r * I.ld + g * 8, I.cols - g * 8, v, g > 0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, finite_bits(v[i]));
         }
@@ -105,7 +119,7 @@ __global__ void __launch_bounds__(PREP_THREADS) prep_operand_kernel(const __grid
         for (int64_t g = threadIdx.x % tx; g < groups; g += tx) {
             float v[8];
             const int64_t left = I.cols - g * 8, at = r * I.dst_ld + g * 8;
-            prep_load8_typed(T.type, I.src, r * I.ld + g * 8, left, v);
+            prep_load8_typed(T.type, I.src, r * I.ld + g * 8, left, v, g > 0);
             if (planes) {
                 float l[8];
 #pragma unroll
@@ -153,7 +167,7 @@ __global__ void __launch_bounds__(PREP_THREADS) norm_partial_kernel(const __grid
     for (int64_t r = int64_t(blockIdx.x) * ty + threadIdx.x / tx; r < P.rows; r += int64_t(gridDim.x) * ty)
         for (int64_t g = threadIdx.x % tx; g < groups; g += tx) {
             float v[8];
-            prep_load8_typed(P.in_type, P.in, blockIdx.y * P.stride + r * P.ld + g * 8, P.cols - g * 8, v);
+            prep_load8_typed(P.in_type, P.in, blockIdx.y * P.stride + r * P.ld + g * 8, P.cols - g * 8, v, g > 0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s += double(v[i]) * double(v[i]);
         }
@@ -187,7 +201,7 @@ __global__ void __launch_bounds__(PREP_THREADS) norm_apply_kernel(const __grid_c
         for (int64_t g = threadIdx.x % tx; g < groups; g += tx) {
             float v[8];
             const int64_t left = P.cols - g * 8;
-            prep_load8_typed(P.in_type, P.in, blockIdx.y * P.stride + r * P.ld + g * 8, left, v);
+            prep_load8_typed(P.in_type, P.in, blockIdx.y * P.stride + r * P.ld + g * 8, left, v, g > 0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = float(double(v[i]) * f);
             if (P.planes) {

@@ -5,11 +5,13 @@
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
 #include <utility>
 
+#include "ffn_tokens.cuh"
 #include "layer_norm.cuh"
 #include "ns_small.cuh"
 #include "operand_prep.cuh"
@@ -260,14 +262,14 @@ bool block_map(scalecom_ops* o, CUtensorMap* map, const Surface& a, int32_t* tma
                      e == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-bool set_out(scalecom_ops* o, TcParams& P, int k, const Surface& a) {
+bool set_out(scalecom_ops* o, TcJob& P, int k, const Surface& a) {
     P.out[k].base = static_cast<char*>(const_cast<void*>(a.p));
     P.out[k].ld = a.ld;
     P.out[k].plane = a.plane;
     P.out[k].batch = a.stride;
     return block_map(o, &P.o[k], a, &P.out[k].tma);
 }
-bool set_in(scalecom_ops* o, TcParams& P, const Surface& a) {
+bool set_in(scalecom_ops* o, TcMore& P, const Surface& a) {
     P.in = a.p;
     P.in_ld = a.ld;
     P.in_plane = a.plane;
@@ -328,21 +330,23 @@ int64_t product_iters(const Product& p) {
     return ceil_div(p.k, TC_BK) * (p.a2 ? 2 : 1);
 }
 
-template <int BN, int EPI, int PL, int CG>
-cudaError_t tc_launch(scalecom_ops* o, const TcParams& P) {
-    const int64_t units = int64_t(P.batch) * P.tiles * P.splits, slots = o->sms / CG;
-    return launch_cluster(o, CG, tc_product_kernel<BN, EPI, PL, CG>, dim3(unsigned((units < slots ? units : slots) * CG)), TC_THREADS,
+template <int BN, int EPI, int PL, int CG, int NJ>
+cudaError_t tc_launch(scalecom_ops* o, const TcParams<NJ>& P) {
+    int64_t units = 0;
+    for (int j = 0; j < P.jobs; ++j) units += int64_t(P.job[j].batch) * P.job[j].tiles * P.job[j].splits;
+    const int64_t slots = o->sms / CG;
+    return launch_cluster(o, CG, tc_product_kernel<BN, EPI, PL, CG, NJ>, dim3(unsigned((units < slots ? units : slots) * CG)), TC_THREADS,
                           TcShape<BN, EPI, PL, CG>::SMEM, P);
 }
 template <int EPI>
-cudaError_t tc_launch_any(scalecom_ops* o, const Plan& pl, int planes, const TcParams& P) {
+cudaError_t tc_launch_any(scalecom_ops* o, const Plan& pl, int planes, const TcParams<1>& P) {
     if (planes > 1) return pl.cg == 2 ? tc_launch<128, EPI, 2, 2>(o, P) : tc_launch<128, EPI, 2, 1>(o, P);
     if (pl.cg == 1) return tc_launch<128, EPI, 1, 1>(o, P);
     return pl.bn == 256 ? tc_launch<256, EPI, 1, 2>(o, P) : tc_launch<128, EPI, 1, 2>(o, P);
 }
-template <int BN, int EPI, int PL, int CG>
+template <int BN, int EPI, int PL, int CG, int NJ = 1>
 cudaError_t tc_attribute() {
-    return cudaFuncSetAttribute(tc_product_kernel<BN, EPI, PL, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, EPI, PL, CG>::SMEM);
+    return cudaFuncSetAttribute(tc_product_kernel<BN, EPI, PL, CG, NJ>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, EPI, PL, CG>::SMEM);
 }
 template <int EPI>
 cudaError_t tc_attributes() {
@@ -360,48 +364,105 @@ size_t split_bytes(const scalecom_ops* o, int epi, const Product& p) {
     return pl.splits > 1 ? size_t(pl.tiles) * p.batch * pl.splits * pl.cg * TC_BM * pl.bn * 4 : 0;
 }
 
-// P: the epilogue's fields are set by the caller
-int run_product(scalecom_ops* o, int epi, const Product& p, TcParams& P, float* partial) {
-    const Plan pl = make_plan(o, epi, p.a->planes, p.m, p.n, product_iters(p), p.batch);
+// Everything of a product but its epilogue's fields, which the caller sets.
+int set_job(scalecom_ops* o, int epi, const Product& p, const Plan& pl, TcJob& J) {
     if (pl.tiles * p.batch > 0x7FFFFFFFll / 32) return SCALECOM_ERR_INVALID_ARG;
     const int bbox = epi == EPI_GATE ? pl.bn / 2 : pl.bn / pl.cg;      // rows of B that one copy brings
-    bool ok = encode(o, &P.a[0], *p.a, p.bf16, p.a_mn, TC_BM) && encode(o, &P.b[0], *p.b, p.bf16, p.b_mn, bbox);
-    if (ok && p.a2) ok = encode(o, &P.a[1], *p.a2, p.bf16, p.a_mn, TC_BM);
-    if (ok && p.b2) ok = encode(o, &P.b[1], *p.b2, p.bf16, p.b_mn, bbox);
+    bool ok = encode(o, &J.a[0], *p.a, p.bf16, p.a_mn, TC_BM) && encode(o, &J.b[0], *p.b, p.bf16, p.b_mn, bbox);
+    if (ok && p.a2) ok = encode(o, &J.a[1], *p.a2, p.bf16, p.a_mn, TC_BM);
+    if (ok && p.b2) ok = encode(o, &J.b[1], *p.b2, p.bf16, p.b_mn, bbox);
     if (!ok) return SCALECOM_ERR_CUDA;
-    P.pairs = p.a2 ? 2 : 1;
-    P.kblocks = int32_t(ceil_div(p.k, TC_BK));
-    P.m = int32_t(p.m);
-    P.n = int32_t(p.n);
-    P.mt = int32_t(pl.mt);
-    P.nt = int32_t(pl.nt);
-    P.tiles = int32_t(pl.tiles);
-    P.batch = p.batch;
-    P.splits = pl.splits;
-    P.a_mn = p.a_mn;
-    P.b_mn = p.b_mn;
-    P.a_batched = p.a_batched;
-    P.b_batched = p.b_batched;
+    J.pairs = p.a2 ? 2 : 1;
+    J.kblocks = int32_t(ceil_div(p.k, TC_BK));
+    J.m = int32_t(p.m);
+    J.n = int32_t(p.n);
+    J.mt = int32_t(pl.mt);
+    J.nt = int32_t(pl.nt);
+    J.tiles = int32_t(pl.tiles);
+    J.batch = p.batch;
+    J.splits = pl.splits;
+    J.a_mn = p.a_mn;
+    J.b_mn = p.b_mn;
+    J.a_batched = p.a_batched;
+    J.b_batched = p.b_batched;
     // fp32 accumulators; both operands fp16 (0) or bf16 (1); majors; N / 8, M / 16
-    P.idesc = (1u << 4) | ((p.bf16 ? 1u : 0u) << 7) | ((p.bf16 ? 1u : 0u) << 10) | ((p.a_mn ? 1u : 0u) << 15) |
+    J.idesc = (1u << 4) | ((p.bf16 ? 1u : 0u) << 7) | ((p.bf16 ? 1u : 0u) << 10) | ((p.a_mn ? 1u : 0u) << 15) |
               ((p.b_mn ? 1u : 0u) << 16) | (uint32_t(pl.bn / 8) << 17) | (uint32_t(TC_BM * pl.cg / 16) << 24);
+    J.amax_a = p.a->amax;
+    J.amax_b = p.b->amax;
+    return SCALECOM_OK;
+}
+
+// P: the epilogue's fields are set by the caller
+int run_product(scalecom_ops* o, int epi, const Product& p, TcParams<1>& P, float* partial) {
+    const Plan pl = make_plan(o, epi, p.a->planes, p.m, p.n, product_iters(p), p.batch);
+    const int rc = set_job(o, epi, p, pl, P.job[0]);
+    if (rc != SCALECOM_OK) return rc;
+    P.jobs = 1;
     P.status = o->ctrl;
     P.partial = partial;
     P.arrived = o->ctrl + 16;
-    P.amax_a = p.a->amax;
-    P.amax_b = p.b->amax;
     cudaError_t e;
+    const int planes = p.a->planes;
     switch (epi) {
-        case EPI_STORE: e = tc_launch_any<EPI_STORE>(o, pl, p.a->planes, P); break;
-        case EPI_GATE: e = tc_launch_any<EPI_GATE>(o, pl, p.a->planes, P); break;
-        case EPI_GATE_BWD: e = tc_launch_any<EPI_GATE_BWD>(o, pl, p.a->planes, P); break;
-        case EPI_GRAM: e = tc_launch_any<EPI_GRAM>(o, pl, p.a->planes, P); break;
-        case EPI_POLY: e = tc_launch_any<EPI_POLY>(o, pl, p.a->planes, P); break;
-        default: e = tc_launch_any<EPI_PLANES>(o, pl, p.a->planes, P); break;
+        case EPI_STORE: e = tc_launch_any<EPI_STORE>(o, pl, planes, P); break;
+        case EPI_GATE: e = tc_launch_any<EPI_GATE>(o, pl, planes, P); break;
+        case EPI_GATE_BWD: e = tc_launch_any<EPI_GATE_BWD>(o, pl, planes, P); break;
+        case EPI_GRAM: e = tc_launch_any<EPI_GRAM>(o, pl, planes, P); break;
+        case EPI_POLY: e = tc_launch_any<EPI_POLY>(o, pl, planes, P); break;
+        default: e = tc_launch_any<EPI_PLANES>(o, pl, planes, P); break;
     }
     if (e != cudaSuccess) {
         cudaGetLastError();
         return SCALECOM_ERR_CUDA;
+    }
+    return SCALECOM_OK;
+}
+
+// Up to four independent stores. Where together they fill the device without parts of k they are one launch, the longest sums
+// first: their tiles then leave one ragged last wave instead of four, and three launches and fills fewer.
+struct Stored { const Product* p; Surface out; };
+int run_stores(scalecom_ops* o, const Stored* list, int n, float* partial) {
+    if (!n) return SCALECOM_OK;
+    const int planes = list[0].p->a->planes;
+    Plan pl[TC_JOBS];
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) {
+        const Product& p = *list[i].p;
+        pl[i].bn = planes > 1 ? 128 : 256;
+        pl[i].cg = 2;
+        pl[i].splits = 1;
+        pl[i].mt = ceil_div(p.m, 2 * TC_BM);
+        pl[i].nt = ceil_div(p.n, pl[i].bn);
+        pl[i].tiles = pl[i].mt * pl[i].nt;
+        tiles += pl[i].tiles;
+    }
+    if (n > 1 && tiles >= o->sms / 2) {
+        TcParams<TC_JOBS> P;
+        std::memset(&P, 0, sizeof P);
+        for (int i = 0; i < n; ++i) {
+            TcJob& J = P.job[i];
+            const int rc = set_job(o, EPI_STORE, *list[i].p, pl[i], J);
+            if (rc != SCALECOM_OK) return rc;
+            J.type = list[i].out.type;
+            J.alpha = 1.0f;
+            if (!set_out(o, J, 0, list[i].out)) return SCALECOM_ERR_CUDA;
+        }
+        P.jobs = n;
+        P.status = o->ctrl;
+        const cudaError_t e = planes > 1 ? tc_launch<128, EPI_STORE, 2, 2>(o, P) : tc_launch<256, EPI_STORE, 1, 2>(o, P);
+        if (e == cudaSuccess) return SCALECOM_OK;
+        cudaGetLastError();
+        return SCALECOM_ERR_CUDA;
+    }
+    for (int i = 0; i < n; ++i) {
+        TcParams<1> P;
+        std::memset(&P, 0, sizeof P);
+        P.job[0].type = list[i].out.type;
+        P.job[0].alpha = 1.0f;
+        if (!set_out(o, P.job[0], 0, list[i].out)) return SCALECOM_ERR_CUDA;
+        const int rc = run_product(o, EPI_STORE, *list[i].p, P, partial);
+        if (rc != SCALECOM_OK) return rc;
     }
     return SCALECOM_OK;
 }
@@ -451,7 +512,58 @@ struct FfnArgs {
     int64_t ldx;
 };
 
+template <typename T, int VEC, bool GATE>
+cudaError_t tokens_launch(scalecom_ops* o, FtParams P) {
+    // warps to a row: enough for 16 warps a multiprocessor where there are few rows
+    P.split = 1;
+    while (P.split < FT_WARPS && int64_t(P.rows) * P.split < int64_t(o->sms) * 16 && P.k / (P.split * 2) >= 32 * VEC) P.split *= 2;
+    const dim3 grid(unsigned(ceil_div(P.rows, FT_WARPS / P.split)));
+    if (P.tokens == 1) return launch(o, ffn_tokens_kernel<T, VEC, 1, GATE>, grid, FT_THREADS, 0, P);
+    if (P.tokens == 2) return launch(o, ffn_tokens_kernel<T, VEC, 2, GATE>, grid, FT_THREADS, 0, P);
+    if (P.tokens <= 4) return launch(o, ffn_tokens_kernel<T, VEC, 4, GATE>, grid, FT_THREADS, 0, P);
+    return launch(o, ffn_tokens_kernel<T, VEC, 8, GATE>, grid, FT_THREADS, 0, P);
+}
+template <typename T>
+int ffn_tokens(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* saved) {
+    constexpr int V = 16 / sizeof(T);
+    const int64_t fp = pad8(A.hidden);
+    int rc = ensure_ws(o, size_t(A.tokens) * fp * sizeof(T));
+    if (rc != SCALECOM_OK) return rc;
+    auto on_grid = [](const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % V == 0; };
+    FtParams P;
+    std::memset(&P, 0, sizeof P);
+    P.x = A.x; P.w0 = A.wg; P.w1 = A.wu; P.out = o->ws; P.saved = saved;
+    P.ldx = A.ldx; P.ldo = fp;
+    P.tokens = int32_t(A.tokens); P.rows = int32_t(A.hidden); P.k = int32_t(A.width); P.act = A.act;
+    const bool v1 = on_grid(A.x, A.ldx) && on_grid(A.wg, A.width) && on_grid(A.wu, A.width);
+    cudaError_t e = v1 ? tokens_launch<T, V, true>(o, P) : tokens_launch<T, 1, true>(o, P);
+    if (e != cudaSuccess) return SCALECOM_ERR_CUDA;
+    P.x = o->ws; P.w0 = A.wd; P.w1 = nullptr; P.out = y; P.saved = nullptr;
+    P.ldx = fp; P.ldo = ldy;
+    P.rows = int32_t(A.width); P.k = int32_t(A.hidden);
+    e = on_grid(A.wd, A.hidden) ? tokens_launch<T, V, false>(o, P) : tokens_launch<T, 1, false>(o, P);
+    return e == cudaSuccess ? SCALECOM_OK : SCALECOM_ERR_CUDA;
+}
+
+// Whether the rows-at-a-time kernels are the faster ones. Beyond what both spend on launches they take, measured in us for a MB of
+// weights, 0.07 + 0.13 t (16 bits) or 0.05 + 0.10 t (fp32) for t tokens -- 0.5 t and 0.23 t off the 16-byte grid -- against 0.19 and
+// 0.75 of the tensor-core path (0.4 and 0.9), whose launches and fills take some 15 us more (45 with two planes).
+bool few_tokens(const FfnArgs& A) {
+    if (A.tokens > FT_MOST) return false;
+    const bool f32 = A.type == SCALECOM_F32;
+    const int64_t grid = f32 ? 4 : 8;
+    const bool vec = A.width % grid == 0 && A.hidden % grid == 0 &&
+                     ((reinterpret_cast<uintptr_t>(A.wg) | reinterpret_cast<uintptr_t>(A.wu) | reinterpret_cast<uintptr_t>(A.wd)) & 15u) == 0;
+    const double mb = 3e-6 * double(A.width) * double(A.hidden) * double(type_size(A.type)), t = double(A.tokens);
+    const double rows = f32 ? (vec ? 0.05 + 0.10 * t : 0.23 * t) : (vec ? 0.07 + 0.13 * t : 0.5 * t);
+    const double tiles = f32 ? (vec ? 0.75 : 0.9) : (vec ? 0.19 : 0.4);
+    return mb * (rows - tiles) < (f32 ? 45.0 : vec ? 15.0 : 25.0);
+}
+
 int ffn_forward(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* saved) {
+    if (few_tokens(A))
+        return A.type == SCALECOM_F32 ? ffn_tokens<float>(o, A, y, ldy, saved)
+             : A.type == SCALECOM_F16 ? ffn_tokens<__half>(o, A, y, ldy, saved) : ffn_tokens<__nv_bfloat16>(o, A, y, ldy, saved);
     const bool f32 = A.type == SCALECOM_F32, bf16 = A.type == SCALECOM_BF16;
     const int64_t T = A.tokens, d = A.width, f = A.hidden, fp = pad8(f);
     for (int pass = 0; pass < 2; ++pass) {
@@ -486,29 +598,29 @@ int ffn_forward(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* s
         if (f32 && cudaMemsetAsync(am, 0, AM_WORDS * 4, o->stream) != cudaSuccess) return SCALECOM_ERR_CUDA;
         int rc = prep.run(o, true);
         if (rc != SCALECOM_OK) return rc;
-        TcParams P;
+        TcParams<1> P;
         std::memset(&P, 0, sizeof P);
-        P.type = A.type;
-        P.act = A.act;
-        P.alpha = 1.0f;
+        P.job[0].type = A.type;
+        P.more.act = A.act;
+        P.job[0].alpha = 1.0f;
         Surface hs, ss;
         hs.p = h; hs.type = A.type; hs.rows = T; hs.cols = f; hs.ld = fp;
-        bool ok = set_out(o, P, 0, hs);
+        bool ok = set_out(o, P.job[0], 0, hs);
         if (saved) {
             ss.p = saved; ss.type = A.type; ss.rows = T; ss.cols = f; ss.ld = f; ss.planes = 2; ss.plane = T * f;
-            ok = ok && set_out(o, P, 1, ss);
+            ok = ok && set_out(o, P.job[0], 1, ss);
         }
         if (!ok) return SCALECOM_ERR_CUDA;
-        P.amax_o = f32 ? am + AM_H : nullptr;
+        P.more.amax_o = f32 ? am + AM_H : nullptr;
         rc = run_product(o, EPI_GATE, up, P, partial);
         if (rc == SCALECOM_OK) rc = prep_h.run(o, false);
         if (rc != SCALECOM_OK) return rc;
         std::memset(&P, 0, sizeof P);
-        P.type = A.type;
-        P.alpha = 1.0f;
+        P.job[0].type = A.type;
+        P.job[0].alpha = 1.0f;
         Surface ys;
         ys.p = y; ys.type = A.type; ys.rows = T; ys.cols = d; ys.ld = ldy;
-        if (!set_out(o, P, 0, ys)) return SCALECOM_ERR_CUDA;
+        if (!set_out(o, P.job[0], 0, ys)) return SCALECOM_ERR_CUDA;
         return run_product(o, EPI_STORE, down, P, partial);
     }
     return SCALECOM_ERR_INTERNAL;
@@ -571,35 +683,35 @@ int ffn_backward(scalecom_ops* o, const FfnArgs& A, int wgrad_type, const void* 
         if (f32 && cudaMemsetAsync(am, 0, AM_WORDS * 4, o->stream) != cudaSuccess) return SCALECOM_ERR_CUDA;
         int rc = prep.run(o, true);
         if (rc != SCALECOM_OK) return rc;
-        TcParams P;
+        TcParams<1> P;
         std::memset(&P, 0, sizeof P);
-        P.type = A.type;
-        P.act = A.act;
-        P.alpha = 1.0f;
+        P.job[0].type = A.type;
+        P.more.act = A.act;
+        P.job[0].alpha = 1.0f;
         Surface ss, ms;
         ss.p = saved; ss.type = A.type; ss.rows = T; ss.cols = f; ss.ld = f; ss.planes = 2; ss.plane = T * f;
         ms.p = mid; ms.type = A.type; ms.rows = T; ms.cols = f; ms.ld = fp; ms.planes = 3; ms.plane = T * fp;
-        if (!set_in(o, P, ss) || !set_out(o, P, 0, ms)) return SCALECOM_ERR_CUDA;
-        P.amax_o = f32 ? am + AM_DGU : nullptr;
-        P.amax_o2 = f32 ? am + AM_H : nullptr;
+        if (!set_in(o, P.more, ss) || !set_out(o, P.job[0], 0, ms)) return SCALECOM_ERR_CUDA;
+        P.more.amax_o = f32 ? am + AM_DGU : nullptr;
+        P.more.amax_o2 = f32 ? am + AM_H : nullptr;
         rc = run_product(o, EPI_GATE_BWD, pdh, P, partial);
         if (rc == SCALECOM_OK) rc = prep_mid.run(o, false);
         if (rc != SCALECOM_OK) return rc;
-        auto store = [&](const Product& p, void* out, int type, int64_t ld) -> int {
-            TcParams Q;
-            std::memset(&Q, 0, sizeof Q);
-            Q.type = type;
-            Q.alpha = 1.0f;
-            Surface os;
+        Stored list[TC_JOBS];
+        int n = 0;
+        auto add = [&](const Product& p, void* out, int type, int64_t ld) {
+            if (!out) return;
+            Surface& os = list[n].out;
+            os = Surface();
             os.p = out; os.type = type; os.rows = p.m; os.cols = p.n; os.ld = ld;
-            if (!set_out(o, Q, 0, os)) return SCALECOM_ERR_CUDA;
-            return run_product(o, EPI_STORE, p, Q, partial);
+            list[n++].p = &p;
         };
-        if (dx) rc = store(pdx, dx, A.type, lddx);
-        if (rc == SCALECOM_OK && dwg) rc = store(pwg, dwg, wgrad_type, d);
-        if (rc == SCALECOM_OK && dwu) rc = store(pwu, dwu, wgrad_type, d);
-        if (rc == SCALECOM_OK && dwd) rc = store(pwd, dwd, wgrad_type, f);
-        return rc;
+        add(pdx, dx, A.type, lddx);
+        add(pwg, dwg, wgrad_type, d);
+        add(pwu, dwu, wgrad_type, d);
+        add(pwd, dwd, wgrad_type, f);
+        std::stable_sort(list, list + n, [](const Stored& a, const Stored& b) { return product_iters(*a.p) > product_iters(*b.p); });
+        return run_stores(o, list, n, partial);
     }
     return SCALECOM_ERR_INTERNAL;
 }
@@ -755,30 +867,30 @@ int orthogonalise(scalecom_ops* o, const NsArgs& A) {
         for (int s = 0; s < A.steps; ++s) {
             const float* co = A.co + (A.ncoef > 1 ? 3 * s : 0);
             const Operand *now = &x[s & 1], *next = &x[(s & 1) ^ 1];
-            TcParams P;
+            TcParams<1> P;
             std::memset(&P, 0, sizeof P);
             gram.a = gram.b = now;
-            P.alpha = float(1.0 / NS_SCALE);
-            if (!set_out(o, P, 0, surface(g))) return SCALECOM_ERR_CUDA;
+            P.job[0].alpha = float(1.0 / NS_SCALE);
+            if (!set_out(o, P.job[0], 0, surface(g))) return SCALECOM_ERR_CUDA;
             int rc = run_product(o, EPI_GRAM, gram, P, partial);
             if (rc != SCALECOM_OK) return rc;
             std::memset(&P, 0, sizeof P);
-            P.poly_a = float(co[0] * NS_SCALE); P.poly_b = co[1]; P.poly_c = float(co[2] / NS_SCALE);
-            if (!set_in(o, P, surface(g)) || !set_out(o, P, 0, surface(q))) return SCALECOM_ERR_CUDA;
+            P.more.poly_a = float(co[0] * NS_SCALE); P.more.poly_b = co[1]; P.more.poly_c = float(co[2] / NS_SCALE);
+            if (!set_in(o, P.more, surface(g)) || !set_out(o, P.job[0], 0, surface(q))) return SCALECOM_ERR_CUDA;
             rc = run_product(o, EPI_POLY, poly, P, partial);
             if (rc != SCALECOM_OK) return rc;
             std::memset(&P, 0, sizeof P);
             (tall ? apply.a : apply.b) = now;
             if (s + 1 < A.steps) {
-                P.alpha = float(1.0 / NS_SCALE);
-                if (!set_out(o, P, 0, surface(*next))) return SCALECOM_ERR_CUDA;
+                P.job[0].alpha = float(1.0 / NS_SCALE);
+                if (!set_out(o, P.job[0], 0, surface(*next))) return SCALECOM_ERR_CUDA;
                 rc = run_product(o, EPI_PLANES, apply, P, partial);
             } else {
-                P.alpha = float(double(A.scale) / (NS_SCALE * NS_SCALE));
-                P.type = A.out_type;
+                P.job[0].alpha = float(double(A.scale) / (NS_SCALE * NS_SCALE));
+                P.job[0].type = A.out_type;
                 Surface os;
                 os.p = A.out; os.type = A.out_type; os.rows = A.rows; os.cols = A.cols; os.ld = A.ld_out; os.batch = int(B); os.stride = A.out_stride;
-                if (!set_out(o, P, 0, os)) return SCALECOM_ERR_CUDA;
+                if (!set_out(o, P.job[0], 0, os)) return SCALECOM_ERR_CUDA;
                 rc = run_product(o, EPI_STORE, apply, P, partial);
             }
             if (rc != SCALECOM_OK) return rc;
@@ -813,6 +925,8 @@ int scalecom_ops_create(scalecom_ops** out) {
         o->encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled>(fn);
     }
     if (e == cudaSuccess) e = tc_attributes<EPI_STORE>();
+    if (e == cudaSuccess) e = tc_attribute<256, EPI_STORE, 1, 2, TC_JOBS>();
+    if (e == cudaSuccess) e = tc_attribute<128, EPI_STORE, 2, 2, TC_JOBS>();
     if (e == cudaSuccess) e = tc_attributes<EPI_GATE>();
     if (e == cudaSuccess) e = tc_attributes<EPI_GATE_BWD>();
     if (e == cudaSuccess) e = tc_attributes<EPI_GRAM>();

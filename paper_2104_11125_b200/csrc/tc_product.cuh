@@ -64,30 +64,39 @@ struct TcOut {
     int32_t tma;                              // 16-byte grid: through the tensor map
 };
 
-struct TcParams {
+// one product of a launch
+struct TcJob {
     CUtensorMap a[2], b[2];
+    CUtensorMap o[2];                         // outputs in blocks of 32 x 32
+    TcOut out[2];                             // STORE: out; GATE: h, saved; GATE_BWD: {dg, du, h}; Newton-Schulz: planes
     int32_t pairs, kblocks;                   // products that are summed (1 or 2), 64-wide blocks of k in each
     int32_t m, n;                             // extent of the result (EPI_GATE: n counts gate columns)
     int32_t mt, nt, tiles;                    // tiles of one matrix
     int32_t batch, splits;
     int32_t a_mn, b_mn, a_batched, b_batched;
     uint32_t idesc;
-    uint32_t* status;
-    float* partial;                           // splits > 1: [batch*tiles][blocks of a tile][splits][BN][128] accumulators
-    uint32_t* arrived;                        // splits > 1: [batch*tiles][blocks of a tile], zero between launches
-
-    // epilogue
-    CUtensorMap o[2], i;                      // outputs and input in blocks of 32 x 32
-    TcOut out[2];                             // STORE: out; GATE: h, saved; GATE_BWD: {dg, du, h}; Newton-Schulz: planes
+    int32_t type;                             // element type of the outputs and of saved
+    float alpha;
+    const uint32_t *amax_a, *amax_b;          // largest magnitudes behind the operands' scales, NULL: unscaled
+};
+constexpr int TC_JOBS = 4;
+// what the epilogues other than STORE read besides
+struct TcMore {
+    CUtensorMap i;
     const void* in;                           // GATE_BWD: saved; POLY: the planes of A
     int64_t in_ld, in_plane, in_batch;
     int32_t in_tma;
-    int32_t type;                             // element type of the outputs and of saved
     int32_t act;
-    float alpha;
-    const uint32_t *amax_a, *amax_b;          // largest magnitudes behind the operands' scales, NULL: unscaled
     uint32_t *amax_o, *amax_o2;               // fp32 intermediates: their largest magnitude is collected
     float poly_a, poly_b, poly_c;
+};
+template <int NJ> struct TcParams {
+    TcJob job[NJ];                            // independent products, worked on one after another as one list of tiles
+    TcMore more;
+    int32_t jobs;
+    uint32_t* status;
+    float* partial;                           // splits > 1: [batch*tiles][blocks of a tile][splits][BN][128] accumulators
+    uint32_t* arrived;                        // splits > 1: [batch*tiles][blocks of a tile], zero between launches
 };
 
 // ---- mbarriers, TMA, tcgen05 -------------------------------------------------------------------------
@@ -312,21 +321,28 @@ __device__ __forceinline__ void gate_back_row(float (&g)[32], float (&v)[32], fl
     }
 
 // ---- tile order ----------------------------------------------------------------------------------------
-struct TcUnit { int batch, mt, nt, split, tile; };
+struct TcUnit { int job, batch, mt, nt, split, tile; };
 
-template <int BN, int EPI, int BM>
-__device__ __forceinline__ TcUnit tc_unit(const TcParams& P, int u) {
+template <int BN, int EPI, int BM, int NJ>
+__device__ __forceinline__ TcUnit tc_unit(const TcParams<NJ>& P, int u) {
     TcUnit r;
-    r.split = u % P.splits;
-    u /= P.splits;
+    r.job = 0;
+    if (NJ > 1)
+        while (r.job + 1 < P.jobs && u >= P.job[r.job].batch * P.job[r.job].tiles * P.job[r.job].splits) {
+            u -= P.job[r.job].batch * P.job[r.job].tiles * P.job[r.job].splits;
+            ++r.job;
+        }
+    const TcJob& J = P.job[r.job];
+    r.split = u % J.splits;
+    u /= J.splits;
     r.tile = u;                                   // over all matrices
-    r.batch = u / P.tiles;
-    int t = u % P.tiles;
+    r.batch = u / J.tiles;
+    int t = u % J.tiles;
     if (EPI == EPI_GRAM || EPI == EPI_POLY) {     // symmetric result: tiles that touch the lower triangle
         int mt = 0;
         for (;; ++mt) {
             int cols = (mt * BM + BM - 1) / BN + 1;
-            if (cols > P.nt) cols = P.nt;
+            if (cols > J.nt) cols = J.nt;
             if (t < cols) break;
             t -= cols;
         }
@@ -334,13 +350,18 @@ __device__ __forceinline__ TcUnit tc_unit(const TcParams& P, int u) {
         r.nt = t;
     } else {                                      // bands of 2048 rows, column by column: the band's A stays in L2
         constexpr int BAND = 2048 / BM;
-        const int band = t / (BAND * P.nt), first = band * BAND;
-        const int rows = P.mt - first < BAND ? P.mt - first : BAND;
-        const int in = t - band * BAND * P.nt;
+        const int band = t / (BAND * J.nt), first = band * BAND;
+        const int rows = J.mt - first < BAND ? J.mt - first : BAND;
+        const int in = t - band * BAND * J.nt;
         r.nt = in / rows;
         r.mt = first + in % rows;
     }
     return r;
+}
+template <int NJ> __device__ __forceinline__ int tc_units(const TcParams<NJ>& P) {
+    int n = 0;
+    for (int j = 0; j < (NJ > 1 ? P.jobs : 1); ++j) n += P.job[j].batch * P.job[j].tiles * P.job[j].splits;
+    return n;
 }
 
 // ---- blocks of 32 x 32 on their way out and in ----------------------------------------------------------------
@@ -364,21 +385,21 @@ __device__ __forceinline__ uint32_t ring_next(Ring& r) {
 }
 // a staged block to global memory at (row0, col0)
 template <int BYTES>
-__device__ __forceinline__ void ring_send(const TcParams& P, int k, uint32_t slot, int row0, int col0, int plane, int batch) {
-    const TcOut& o = P.out[k];
+__device__ __forceinline__ void ring_send(const TcJob& J, int k, uint32_t slot, int row0, int col0, int plane, int batch) {
+    const TcOut& o = J.out[k];
     if (o.tma) {
         fence_async_smem();
         __syncwarp();
         if (lane_id() == 0) {
-            tma_store(&P.o[k], col0, row0, plane, batch, slot);
+            tma_store(&J.o[k], col0, row0, plane, batch, slot);
             bulk_commit();
         }
     } else {
         __syncwarp();
         const uint32_t lane = lane_id();
-        const int rows = min(32, P.m - row0);
+        const int rows = min(32, J.m - row0);
         const int64_t at = int64_t(batch) * o.batch + int64_t(plane) * o.plane + int64_t(row0) * o.ld + col0 + lane;
-        if (col0 + int(lane) < P.n) {
+        if (col0 + int(lane) < J.n) {
 #pragma unroll 4
             for (int r = 0; r < rows; ++r) {
                 if (BYTES == 2) reinterpret_cast<uint16_t*>(o.base)[at + r * o.ld] = lds16(slot + piece16(r, lane >> 3) + (lane & 7u) * 2);
@@ -411,22 +432,22 @@ __device__ __forceinline__ void stage16(uint32_t slot, int type, const float (&v
     for (int i = 0; i < 4; ++i) sts128(slot + piece16(lane, i), p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
 }
 template <bool MAY_F32>
-__device__ __forceinline__ void emit(const TcParams& P, int k, Ring& ring, int type, const float (&v)[32], int row0, int col0, int plane, int batch) {
+__device__ __forceinline__ void emit(const TcJob& J, int k, Ring& ring, int type, const float (&v)[32], int row0, int col0, int plane, int batch) {
     if (MAY_F32 && type == SCALECOM_F32) {
         const uint32_t slot = ring_next<4>(ring), lane = lane_id();
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             sts128(slot + piece32(lane, i), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-        ring_send<4>(P, k, slot, row0, col0, plane, batch);
+        ring_send<4>(J, k, slot, row0, col0, plane, batch);
     } else {
         const uint32_t slot = ring_next<2>(ring);
         stage16(slot, type, v);
-        ring_send<2>(P, k, slot, row0, col0, plane, batch);
+        ring_send<2>(J, k, slot, row0, col0, plane, batch);
     }
 }
 // fp16 planes of a block, and with MIRROR of its transpose at (col0, row0)
 template <int PL, bool MIRROR>
-__device__ __forceinline__ void emit_planes(const TcParams& P, Ring& ring, float (&v)[32], int row0, int col0, int batch) {
+__device__ __forceinline__ void emit_planes(const TcJob& J, Ring& ring, float (&v)[32], int row0, int col0, int batch) {
     const uint32_t lane = lane_id();
 #pragma unroll
     for (int pl = 0; pl < PL; ++pl) {
@@ -438,13 +459,13 @@ __device__ __forceinline__ void emit_planes(const TcParams& P, Ring& ring, float
                 v[i] = __half2float(l);
             }
         }
-        emit<false>(P, 0, ring, SCALECOM_F16, v, row0, col0, pl, batch);
+        emit<false>(J, 0, ring, SCALECOM_F16, v, row0, col0, pl, batch);
         if (MIRROR && col0 != row0) {
             const uint32_t slot = ring_next<2>(ring);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 sts16(slot + piece16(i, lane >> 3) + (lane & 7u) * 2, __half_as_ushort(__float2half_rn(v[i])));
-            ring_send<2>(P, 0, slot, col0, row0, pl, batch);
+            ring_send<2>(J, 0, slot, col0, row0, pl, batch);
         }
     }
 }
@@ -496,99 +517,99 @@ struct Inflow {
     bool pending;
 };
 template <int EPI>
-__device__ __forceinline__ bool block_used(const TcParams& P, int row0, int col0) {
-    return row0 < P.m && col0 < P.n && (!(EPI == EPI_GRAM || EPI == EPI_POLY) || col0 <= row0);
+__device__ __forceinline__ bool block_used(const TcJob& J, int row0, int col0) {
+    return row0 < J.m && col0 < J.n && (!(EPI == EPI_GRAM || EPI == EPI_POLY) || col0 <= row0);
 }
 template <int EPI>
-__device__ __forceinline__ void inflow_start(const TcParams& P, Inflow& f, int row0, int col0, int batch) {
-    if (!P.in_tma || f.pending || !block_used<EPI>(P, row0, col0)) return;
+__device__ __forceinline__ void inflow_start(const TcJob& J, const TcMore& M, Inflow& f, int row0, int col0, int batch) {
+    if (!M.in_tma || f.pending || !block_used<EPI>(J, row0, col0)) return;
     f.pending = true;
     if (lane_id() == 0) {
         mbar_expect(f.bar, EPI == EPI_GATE_BWD ? 4096u : 2048u);
-        tma_load<1>(f.smem, &P.i, col0, row0, 0, batch, f.bar);
-        if (EPI == EPI_GATE_BWD) tma_load<1>(f.smem + 2048u, &P.i, col0, row0, 1, batch, f.bar);
+        tma_load<1>(f.smem, &M.i, col0, row0, 0, batch, f.bar);
+        if (EPI == EPI_GATE_BWD) tma_load<1>(f.smem + 2048u, &M.i, col0, row0, 1, batch, f.bar);
     }
 }
 
 // ---- epilogues on a block of 32 x 32: v (and w) hold this lane's row --------------------------------------------
 template <int EPI, int PL>
-__device__ __forceinline__ bool tc_epilogue(const TcParams& P, const TcUnit& u, int row0, int col0, int col_next, float (&v)[32], float (&w)[32], float un,
-                                            uint32_t& top, uint32_t& top2, Ring& ring, Inflow& in, volatile uint32_t* abort) {
-    if (!block_used<EPI>(P, row0, col0)) return true;
-    const int row = row0 + int(lane_id()), nc = P.n - col0;
-    const bool inside = row < P.m;
+__device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, const TcUnit& u, int row0, int col0, int col_next, float (&v)[32], float (&w)[32], float un,
+                                            uint32_t& top, uint32_t& top2, Ring& ring, Inflow& in, volatile uint32_t* abort, uint32_t* status) {
+    if (!block_used<EPI>(J, row0, col0)) return true;
+    const int row = row0 + int(lane_id()), nc = J.n - col0;
+    const bool inside = row < J.m;
     if (EPI == EPI_STORE) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= un;
-        emit<true>(P, 0, ring, P.type, v, row0, col0, 0, u.batch);
+        emit<true>(J, 0, ring, J.type, v, row0, col0, 0, u.batch);
     } else if (EPI == EPI_GATE) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) { v[i] *= un; w[i] *= un; }
-        if (P.out[1].base) {
-            emit<PL == 2>(P, 1, ring, P.type, v, row0, col0, 0, 0);
-            emit<PL == 2>(P, 1, ring, P.type, w, row0, col0, 1, 0);
+        if (J.out[1].base) {
+            emit<PL == 2>(J, 1, ring, J.type, v, row0, col0, 0, 0);
+            emit<PL == 2>(J, 1, ring, J.type, w, row0, col0, 1, 0);
         }
 #define SC_CALL(ACT) gate_row<ACT>(v, v, w)
-        SC_FOR_ACT(P.act, SC_CALL)
+        SC_FOR_ACT(M.act, SC_CALL)
 #undef SC_CALL
         if (PL == 2) top = max(top, row_top(v, inside ? nc : 0));
-        emit<PL == 2>(P, 0, ring, P.type, v, row0, col0, 0, 0);
+        emit<PL == 2>(J, 0, ring, J.type, v, row0, col0, 0, 0);
     } else if (EPI == EPI_GATE_BWD) {
         float g[32];
-        if (PL == 1 && P.in_tma) {
-            if (!__all_sync(FULL, mbar_wait(in.bar, in.phase, abort, P.status))) return false;
+        if (PL == 1 && M.in_tma) {
+            if (!__all_sync(FULL, mbar_wait(in.bar, in.phase, abort, status))) return false;
             in.phase ^= 1u;
             in.pending = false;
-            take16(in.smem, P.type, g);
-            take16(in.smem + 2048u, P.type, w);
+            take16(in.smem, J.type, g);
+            take16(in.smem + 2048u, J.type, w);
             __syncwarp();
-            if (col_next >= 0) inflow_start<EPI>(P, in, row0, col_next, u.batch);
+            if (col_next >= 0) inflow_start<EPI>(J, M, in, row0, col_next, u.batch);
         } else {
-            const int64_t at = int64_t(row) * P.in_ld + col0;
-            load_typed(P.type, P.in, at, g, inside ? nc : 0);
-            load_typed(P.type, P.in, at + P.in_plane, w, inside ? nc : 0);
+            const int64_t at = int64_t(row) * M.in_ld + col0;
+            load_typed(J.type, M.in, at, g, inside ? nc : 0);
+            load_typed(J.type, M.in, at + M.in_plane, w, inside ? nc : 0);
         }
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= un;
 #define SC_CALL(ACT) gate_back_row<ACT>(g, v, w)
-        SC_FOR_ACT(P.act, SC_CALL)
+        SC_FOR_ACT(M.act, SC_CALL)
 #undef SC_CALL
         if (PL == 2) {
             top = max(top, max(row_top(g, inside ? nc : 0), row_top(w, inside ? nc : 0)));
             top2 = max(top2, row_top(v, inside ? nc : 0));
         }
-        emit<PL == 2>(P, 0, ring, P.type, g, row0, col0, 0, 0);
-        emit<PL == 2>(P, 0, ring, P.type, w, row0, col0, 1, 0);
-        emit<PL == 2>(P, 0, ring, P.type, v, row0, col0, 2, 0);
+        emit<PL == 2>(J, 0, ring, J.type, g, row0, col0, 0, 0);
+        emit<PL == 2>(J, 0, ring, J.type, w, row0, col0, 1, 0);
+        emit<PL == 2>(J, 0, ring, J.type, v, row0, col0, 2, 0);
     } else if (EPI == EPI_PLANES) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= P.alpha;
-        emit_planes<PL, false>(P, ring, v, row0, col0, u.batch);
+        for (int i = 0; i < 32; ++i) v[i] *= J.alpha;
+        emit_planes<PL, false>(J, ring, v, row0, col0, u.batch);
     } else {
         // a symmetric result: blocks up to the diagonal, stored here and mirrored
         if (EPI == EPI_POLY) {
             if (PL == 1) {
-                if (!__all_sync(FULL, mbar_wait(in.bar, in.phase, abort, P.status))) return false;
+                if (!__all_sync(FULL, mbar_wait(in.bar, in.phase, abort, status))) return false;
                 in.phase ^= 1u;
                 in.pending = false;
                 take16(in.smem, SCALECOM_F16, w);
                 __syncwarp();
-                if (col_next >= 0) inflow_start<EPI>(P, in, row0, col_next, u.batch);
+                if (col_next >= 0) inflow_start<EPI>(J, M, in, row0, col_next, u.batch);
             } else {
-                const int64_t at = int64_t(u.batch) * P.in_batch + int64_t(row) * P.in_ld + col0;
-                load_typed(SCALECOM_F16, P.in, at, w, inside ? nc : 0);
+                const int64_t at = int64_t(u.batch) * M.in_batch + int64_t(row) * M.in_ld + col0;
+                load_typed(SCALECOM_F16, M.in, at, w, inside ? nc : 0);
                 float l[32];
-                load_typed(SCALECOM_F16, P.in, at + P.in_plane, l, inside ? nc : 0);
+                load_typed(SCALECOM_F16, M.in, at + M.in_plane, l, inside ? nc : 0);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) w[i] += l[i];
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = P.poly_b * w[i] + P.poly_c * v[i] + (i == row - col0 ? P.poly_a : 0.0f);
+            for (int i = 0; i < 32; ++i) v[i] = M.poly_b * w[i] + M.poly_c * v[i] + (i == row - col0 ? M.poly_a : 0.0f);
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= P.alpha;
+            for (int i = 0; i < 32; ++i) v[i] *= J.alpha;
         }
-        emit_planes<PL, true>(P, ring, v, row0, col0, u.batch);
+        emit_planes<PL, true>(J, ring, v, row0, col0, u.batch);
     }
     return true;
 }
@@ -601,8 +622,8 @@ __device__ __forceinline__ bool epilogue_all(bool ok) {
     return r != 0u;
 }
 
-template <int BN, int EPI, int PL, int CG>
-__global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_constant__ TcParams P) {
+template <int BN, int EPI, int PL, int CG, int NJ>
+__global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_constant__ TcParams<NJ> P) {
     using S = TcShape<BN, EPI, PL, CG>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ alignas(8) uint64_t bars[2 * S::STAGES + 2 * S::ACCS + 1 + TC_EPI_WARPS];
@@ -646,8 +667,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
     chain_wait();
 
     volatile uint32_t* abort = &abort_flag;
-    const int units = P.batch * P.tiles * P.splits;
-    const int iters = P.pairs * P.kblocks;
+    const int units = tc_units(P);
     const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
     if (warp == 0) {
@@ -656,34 +676,36 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             bool ok = true;
             for (int un = first; ok && un < units; un += stride) {
                 const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
-                const int it0 = int(int64_t(iters) * u.split / P.splits), it1 = int(int64_t(iters) * (u.split + 1) / P.splits);
+                const TcJob& J = P.job[NJ > 1 ? u.job : 0];
+                const int iters = J.pairs * J.kblocks;
+                const int it0 = int(int64_t(iters) * u.split / J.splits), it1 = int(int64_t(iters) * (u.split + 1) / J.splits);
                 const int m0 = u.mt * S::BM + int(rank) * TC_BM;
                 const int n0 = EPI == EPI_GATE ? u.nt * (BN / 2) : u.nt * BN + int(rank) * (BN / CG);
-                const int ba = P.a_batched ? u.batch : 0, bb = P.b_batched ? u.batch : 0;
+                const int ba = J.a_batched ? u.batch : 0, bb = J.b_batched ? u.batch : 0;
                 for (int it = it0; it < it1; ++it, ++n_issued) {
                     const int s = n_issued % S::STAGES, round = n_issued / S::STAGES;
                     if (!mbar_wait(empty(s), (round & 1) ^ 1, abort, P.status)) { ok = false; break; }
-                    const int pair = it >= P.kblocks, k0 = (it - pair * P.kblocks) * TC_BK;
+                    const int pair = it >= J.kblocks, k0 = (it - pair * J.kblocks) * TC_BK;
                     const uint32_t a = tiles0 + s * S::STAGE_BYTES, b = a + PL * TC_A_BYTES;
                     const uint32_t bar = CG == 2 ? in_block(full(s), 0) : full(s);
                     if (rank == 0) mbar_expect(full(s), S::STAGE_BYTES * CG);      // both blocks' copies
 #pragma unroll
                     for (int pl = 0; pl < PL; ++pl) {
                         const uint32_t ap = a + pl * TC_A_BYTES, bp = b + pl * S::B_BYTES;
-                        if (P.a_mn) {
-                            for (int j = 0; j < TC_BM / 64; ++j) tma_load<CG>(ap + j * 8192, &P.a[pair], m0 + 64 * j, k0, pl, ba, bar);
+                        if (J.a_mn) {
+                            for (int j = 0; j < TC_BM / 64; ++j) tma_load<CG>(ap + j * 8192, &J.a[pair], m0 + 64 * j, k0, pl, ba, bar);
                         } else {
-                            tma_load<CG>(ap, &P.a[pair], k0, m0, pl, ba, bar);
+                            tma_load<CG>(ap, &J.a[pair], k0, m0, pl, ba, bar);
                         }
                         if (EPI == EPI_GATE && CG == 2) {       // the pair's first block has the gate columns, the second the up columns
-                            tma_load<CG>(bp, &P.b[rank], k0, n0, pl, bb, bar);
+                            tma_load<CG>(bp, &J.b[rank], k0, n0, pl, bb, bar);
                         } else if (EPI == EPI_GATE) {
-                            tma_load<CG>(bp, &P.b[0], k0, n0, pl, bb, bar);
-                            tma_load<CG>(bp + S::B_BYTES / 2, &P.b[1], k0, n0, pl, bb, bar);
-                        } else if (P.b_mn) {
-                            for (int j = 0; j < BN / CG / 64; ++j) tma_load<CG>(bp + j * 8192, &P.b[pair], n0 + 64 * j, k0, pl, bb, bar);
+                            tma_load<CG>(bp, &J.b[0], k0, n0, pl, bb, bar);
+                            tma_load<CG>(bp + S::B_BYTES / 2, &J.b[1], k0, n0, pl, bb, bar);
+                        } else if (J.b_mn) {
+                            for (int j = 0; j < BN / CG / 64; ++j) tma_load<CG>(bp + j * 8192, &J.b[pair], n0 + 64 * j, k0, pl, bb, bar);
                         } else {
-                            tma_load<CG>(bp, &P.b[pair], k0, n0, pl, bb, bar);
+                            tma_load<CG>(bp, &J.b[pair], k0, n0, pl, bb, bar);
                         }
                     }
                 }
@@ -698,7 +720,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             bool ok = true;
             for (int un = first; ok && un < units; un += stride) {
                 const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
-                const int it0 = int(int64_t(iters) * u.split / P.splits), it1 = int(int64_t(iters) * (u.split + 1) / P.splits);
+                const TcJob& J = P.job[NJ > 1 ? u.job : 0];
+                const int iters = J.pairs * J.kblocks;
+                const int it0 = int(int64_t(iters) * u.split / J.splits), it1 = int(int64_t(iters) * (u.split + 1) / J.splits);
                 if (PL == 1) {
                     if (!mbar_wait(tempty(n_acc % S::ACCS), ((n_acc / S::ACCS) & 1) ^ 1, abort, P.status)) { ok = false; break; }
                     tc_fence_after();
@@ -711,14 +735,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     tc_fence_after();
                     const uint32_t d = tmem + (n_acc % S::ACCS) * BN;
                     const uint32_t a = tiles0 + s * S::STAGE_BYTES, b = a + PL * TC_A_BYTES;
-                    const uint32_t step_a = P.a_mn ? 2048 >> 4 : 32 >> 4, step_b = P.b_mn ? 2048 >> 4 : 32 >> 4;
+                    const uint32_t step_a = J.a_mn ? 2048 >> 4 : 32 >> 4, step_b = J.b_mn ? 2048 >> 4 : 32 >> 4;
 #pragma unroll
                     for (int t = 0; t < (PL == 2 ? 3 : 1); ++t) {      // lo hi, hi lo, hi hi
-                        const uint64_t da = tc_desc(a + (PL == 2 && t == 0 ? TC_A_BYTES : 0), P.a_mn);
-                        const uint64_t db = tc_desc(b + (PL == 2 && t == 1 ? S::B_BYTES : 0), P.b_mn);
+                        const uint64_t da = tc_desc(a + (PL == 2 && t == 0 ? TC_A_BYTES : 0), J.a_mn);
+                        const uint64_t db = tc_desc(b + (PL == 2 && t == 1 ? S::B_BYTES : 0), J.b_mn);
 #pragma unroll
                         for (int k = 0; k < TC_BK / 16; ++k)
-                            tc_mma<CG>(d, da + k * step_a, db + k * step_b, P.idesc, (t > 0 || k > 0 || (PL == 2 ? !opens : it > it0)) ? 1u : 0u);
+                            tc_mma<CG>(d, da + k * step_a, db + k * step_b, J.idesc, (t > 0 || k > 0 || (PL == 2 ? !opens : it > it0)) ? 1u : 0u);
                     }
                     tc_commit<CG>(empty(s));
                     if (closes) tc_commit<CG>(tfull(n_acc++ % S::ACCS));
@@ -741,18 +765,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             if (rank == 0) mbar_arrive(tempty(i));
             else mbar_arrive_cluster(in_block(tempty(i), 0));
         };
-        float un_scale = P.alpha;
-        if (P.amax_a) un_scale *= plane_unscale(*P.amax_a) * plane_unscale(*P.amax_b);
         uint32_t top = 0u, top2 = 0u;
         int n_acc = 0;
         const uint32_t stage0 = tiles0 + S::STAGES * S::STAGE_BYTES;
         Ring ring = {stage0 + (warp - 4u) * TC_RING, 0};
         Inflow in = {stage0 + TC_EPI_WARPS * TC_RING + (warp - 4u) * S::IN_BYTES, inflow0 + 8u * (warp - 4u), 0u, false};
         auto begin = [&](const TcUnit& u, int row0, int c) {
-            if (S::LOADS && c < CHUNKS) inflow_start<EPI>(P, in, row0, u.nt * WIDTH + chunk(c), u.batch);
+            if (S::LOADS && c < CHUNKS) inflow_start<EPI>(P.job[NJ > 1 ? u.job : 0], P.more, in, row0, u.nt * WIDTH + chunk(c), u.batch);
         };
         for (int un = first; un < units; un += stride) {
             const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
+                const TcJob& J = P.job[NJ > 1 ? u.job : 0];
+                const int iters = J.pairs * J.kblocks;
+            float un_scale = J.alpha;
+            if (J.amax_a) un_scale *= plane_unscale(*J.amax_a) * plane_unscale(*J.amax_b);
             const int row0 = u.mt * S::BM + int(rank) * TC_BM + int(quad) * 32;
             float v[32], w[32];
             float sum[PL == 2 ? BN / 64 : 1][32];       // PL = 2: this thread's columns, in the order of `column`
@@ -760,12 +786,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 if (EPI == EPI_GATE && PL == 2) return (c & 1) * (BN / 2) + (int(half) * (BN / 128) + (c >> 1)) * 32;
                 return int(half) * (BN / 2) + c * 32;
             };
-            if (P.splits == 1) begin(u, row0, 0);
+            if (J.splits == 1) begin(u, row0, 0);
             bool ok = true;
             uint32_t acc = 0;
             int q = 0;
             if (PL == 2) {
-                const int it0 = int(int64_t(iters) * u.split / P.splits), it1 = int(int64_t(iters) * (u.split + 1) / P.splits);
+                const int it0 = int(int64_t(iters) * u.split / J.splits), it1 = int(int64_t(iters) * (u.split + 1) / J.splits);
 #pragma unroll
                 for (int c = 0; c < BN / 64; ++c)
 #pragma unroll
@@ -796,7 +822,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 ++n_acc;
                 acc = tmem + q * BN + lanes;
             }
-            if (P.splits > 1) ok = epilogue_all(ok);       // the block barriers below need every epilogue warp
+            if (J.splits > 1) ok = epilogue_all(ok);       // the block barriers below need every epilogue warp
             if (!ok) break;
             tc_fence_after();
             auto release = [&]() {                          // the accumulator is free once its last columns are in registers
@@ -806,10 +832,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     if (lane == 0) acc_free(q);
                 }
             };
-            if (P.splits > 1) {
+            if (J.splits > 1) {
                 // this part's accumulators to scratch, [column][row]; the block that arrives last adds the parts up in their order
                 const int slot = u.tile * CG + int(rank);
-                float* mine = P.partial + (int64_t(slot) * P.splits) * (TC_BM * BN) + quad * 32 + lane;
+                float* mine = P.partial + (int64_t(slot) * J.splits) * (TC_BM * BN) + quad * 32 + lane;
                 float* put = mine + int64_t(u.split) * (TC_BM * BN);
 #pragma unroll 1
                 for (int c = 0; c < BN / 64; ++c) {
@@ -822,8 +848,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (tid == 0) {
                     const uint32_t before = atomicAdd(&P.arrived[slot], 1u);
-                    last_flag = before + 1u == uint32_t(P.splits);
-                    if (before + 1u == uint32_t(P.splits)) P.arrived[slot] = 0u;
+                    last_flag = before + 1u == uint32_t(J.splits);
+                    if (before + 1u == uint32_t(J.splits)) P.arrived[slot] = 0u;
                     __threadfence();
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -834,7 +860,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 auto gather = [&](int col, float (&x)[32]) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) x[i] = 0.0f;
-                    for (int s = 0; s < P.splits; ++s) {
+                    for (int s = 0; s < J.splits; ++s) {
                         const float* get = mine + int64_t(s) * (TC_BM * BN) + col * TC_BM;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) x[i] += __ldcg(&get[i * TC_BM]);
@@ -846,7 +872,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     gather(at, v);
                     if (EPI == EPI_GATE) gather(BN / 2 + at, w);
                     begin(u, row0, c);
-                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, -1, v, w, un_scale, top, top2, ring, in, abort);
+                    ok = ok && tc_epilogue<EPI, PL>(J, P.more, u, row0, u.nt * WIDTH + at, -1, v, w, un_scale, top, top2, ring, in, abort, P.status);
                 }
             } else {
 #pragma unroll 1
@@ -856,8 +882,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     if (EPI == EPI_GATE) tc_ld32(acc + BN / 2 + at, w);
                     if (c == CHUNKS - 1) release();
                     if (ok) begin(u, row0, c);
-                    ok = ok && tc_epilogue<EPI, PL>(P, u, row0, u.nt * WIDTH + at, c + 1 < CHUNKS ? u.nt * WIDTH + chunk(c + 1) : -1, v, w, un_scale,
-                                                    top, top2, ring, in, abort);
+                    ok = ok && tc_epilogue<EPI, PL>(J, P.more, u, row0, u.nt * WIDTH + at, c + 1 < CHUNKS ? u.nt * WIDTH + chunk(c + 1) : -1, v, w, un_scale,
+                                                    top, top2, ring, in, abort, P.status);
                 }
             }
         }
@@ -866,13 +892,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             bulk_wait_all();                        // the staging area is read, and the results are written, before the block ends
         }
         if (PL == 2 && (EPI == EPI_GATE || EPI == EPI_GATE_BWD)) {
-            if (P.amax_o) {
+            if (P.more.amax_o) {
                 top = __reduce_max_sync(FULL, top);
-                if (lane == 0 && top) atomicMax(P.amax_o, top);
+                if (lane == 0 && top) atomicMax(P.more.amax_o, top);
             }
-            if (P.amax_o2) {
+            if (P.more.amax_o2) {
                 top2 = __reduce_max_sync(FULL, top2);
-                if (lane == 0 && top2) atomicMax(P.amax_o2, top2);
+                if (lane == 0 && top2) atomicMax(P.more.amax_o2, top2);
             }
         }
     }
