@@ -287,8 +287,9 @@ struct Product {
 struct Plan { int bn, cg, splits; int64_t mt, nt, tiles; };
 
 // Tile shape and parts of k: the least estimated time. A tile's 64 k take the tensor core (256 cycles for 128 columns, three
-// times that for two planes) or the SM's 64 bytes a clock from L2, whichever is longer; what a tile adds at its end is only
-// seen once, behind the last wave; a split part costs its accumulators' way through L2.
+// times that for two planes, of which 1,900 cycles become with the sums in registers) or the 53 bytes a clock that an SM was
+// seen to get from L2, whichever is longer; what a tile adds at its end is only
+// seen once, behind the last wave; parts of k cost fences and counting (about 6,000 cycles) and their accumulators' way through L2.
 Plan make_plan(const scalecom_ops* o, int epi, int planes, int64_t m, int64_t n, int64_t iters, int64_t batch) {
     struct Shape { int bn, cg; };
     static const Shape one[] = {{256, 2}, {128, 2}, {128, 1}}, two[] = {{128, 2}, {128, 1}};
@@ -311,11 +312,11 @@ Plan make_plan(const scalecom_ops* o, int epi, int planes, int64_t m, int64_t n,
             }
         }
         const double math = t.bn * 2.0 * (planes > 1 ? 3.0 : 1.0), bytes = planes * (16384.0 + t.bn / t.cg * 128.0);
-        const double block = math > bytes / 64.0 ? math : bytes / 64.0, drain = t.bn * 12.0;
+        const double block = planes > 1 ? 1900.0 : math > bytes / 53.0 ? math : bytes / 53.0, drain = t.bn * 12.0;
         for (int s = 1; s <= 32 && (s == 1 || s * 2 <= iters); ++s) {
             if (s > 1 && p.tiles * batch * t.cg > MAX_SPLIT_TILES) break;
             const double waves = double(ceil_div(p.tiles * batch * s, o->sms / t.cg));
-            const double cost = waves * double(ceil_div(iters, s)) * block + drain + (s > 1 ? (waves + s) * t.bn * 5.0 + 2000.0 : 0.0);
+            const double cost = waves * double(ceil_div(iters, s)) * block + drain + (s > 1 ? (waves * 5.0 + s * 16.0) * t.bn + 6000.0 : 0.0);
             if (cost < least * 0.97) {
                 least = cost;
                 best = p;

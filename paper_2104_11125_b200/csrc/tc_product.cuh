@@ -40,7 +40,10 @@ constexpr int TC_A_BYTES = TC_BM * TC_BK * 2;
 // Staging area of an epilogue warp: two 32 x 32 blocks of 16 bits, or one of 32. What it takes, the operands in flight lack: from a
 // stage's last product to its next data being there takes some 2,800 cycles, so the products run at their rate only with
 // about 190 KB on their way (measured with 8 KB here: five stages of 32 KB, 620 cycles for 64 k that take 512).
+// The gated block's epilogues lay three blocks of 16 bits out and send them together, one fence and one wait for all: sent one by one, each
+// chunk of 32 columns spent some 3,000 of its 6,000 cycles on them.
 constexpr int TC_RING = 4096;
+constexpr int tc_ring(int epi, int planes) { return planes == 1 && (epi == 1 || epi == 2) ? 6144 : TC_RING; }
 constexpr int TC_CHUNK = 1;             // PL = 2: blocks of 64 k between two additions to the sums (two: a fifth faster, and errors of 1e-6 instead of 3.5e-7)
 
 template <int BN, int EPI, int PL, int CG> struct TcShape {
@@ -48,7 +51,8 @@ template <int BN, int EPI, int PL, int CG> struct TcShape {
     static constexpr int STAGE_BYTES = PL * (TC_A_BYTES + B_BYTES);  // A planes, then B planes
     static constexpr bool LOADS = PL == 1 && (EPI == 2 || EPI == 4); // epilogues that read through TMA: 4 KB a warp
     static constexpr int IN_BYTES = LOADS ? 4096 : 0;
-    static constexpr int EPI_BYTES = TC_EPI_WARPS * (TC_RING + IN_BYTES);
+    static constexpr int RING = tc_ring(EPI, PL);
+    static constexpr int EPI_BYTES = TC_EPI_WARPS * (RING + IN_BYTES);
     static constexpr int STAGES = (227 * 1024 - 1024 - 512 - EPI_BYTES) / STAGE_BYTES;
     static constexpr int BM = TC_BM * CG;                            // rows of a tile
     static constexpr int SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 1024;         // + alignment of the swizzle atoms
@@ -203,6 +207,9 @@ __device__ __forceinline__ void tc_ld32(uint32_t addr, float (&v)[32]) {
         : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+#pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
@@ -212,7 +219,6 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, int c0, int c1
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -234,6 +240,33 @@ __device__ __forceinline__ uint32_t lds32(uint32_t at) {
     return v;
 }
 
+// two loads under one wait. The empty statements after it tie the values to it: nothing that uses them can be moved before.
+__device__ __forceinline__ void tc_ld32x2(uint32_t addr0, float (&v)[32], uint32_t addr1, float (&w)[32]) {
+    uint32_t r[2][32];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+            "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+            "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+            : "=r"(r[k][0]), "=r"(r[k][1]), "=r"(r[k][2]), "=r"(r[k][3]), "=r"(r[k][4]), "=r"(r[k][5]), "=r"(r[k][6]), "=r"(r[k][7]),
+              "=r"(r[k][8]), "=r"(r[k][9]), "=r"(r[k][10]), "=r"(r[k][11]), "=r"(r[k][12]), "=r"(r[k][13]), "=r"(r[k][14]), "=r"(r[k][15]),
+              "=r"(r[k][16]), "=r"(r[k][17]), "=r"(r[k][18]), "=r"(r[k][19]), "=r"(r[k][20]), "=r"(r[k][21]), "=r"(r[k][22]), "=r"(r[k][23]),
+              "=r"(r[k][24]), "=r"(r[k][25]), "=r"(r[k][26]), "=r"(r[k][27]), "=r"(r[k][28]), "=r"(r[k][29]), "=r"(r[k][30]), "=r"(r[k][31])
+            : "r"(k ? addr1 : addr0));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+            asm volatile("" : "+r"(r[k][i]), "+r"(r[k][i + 1]), "+r"(r[k][i + 2]), "+r"(r[k][i + 3]), "+r"(r[k][i + 4]), "+r"(r[k][i + 5]),
+                              "+r"(r[k][i + 6]), "+r"(r[k][i + 7]));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        v[i] = __uint_as_float(r[0][i]);
+        w[i] = __uint_as_float(r[1][i]);
+    }
+}
 __device__ __forceinline__ void tc_st32(uint32_t addr, const float (&v)[32]) {
     uint32_t r[32];
 #pragma unroll
@@ -260,22 +293,32 @@ __device__ __forceinline__ uint64_t tc_desc(uint32_t addr, int mn) {
 }
 
 // ---- activations --------------------------------------------------------------------------------------
-// The fast exp and division: 2 + 1.2 |x| units in the last place of fp32 for exp(x), 2 for the quotient, so a sigmoid is within a few
-// units in the last place wherever it is not negligible beside 1 -- below what the products before it lose, and a quarter
-// of the accurate functions' instructions, which set the pace of the backward epilogue.
-__device__ __forceinline__ float act_sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+// The multiplexed unit's 2^x (2 units in the last place) and reciprocal (1): with the rounding of x log2(e), a sigmoid is within a few
+// units in the last place wherever it is not negligible beside 1 -- below what the products before it lose. Results below
+// fp32's normal range are zero. The epilogues are bound by their instructions, and these are four a sigmoid.
+__device__ __forceinline__ float fast_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+constexpr float LOG2_E = 1.4426950408889634f;
+__device__ __forceinline__ float act_sigmoid(float g) { return fast_rcp(1.0f + fast_exp2(-LOG2_E * g)); }
 // value and derivative
 template <int ACT>
 __device__ __forceinline__ void act_both(float g, float& a, float& s) {
     if (ACT == SCALECOM_ACT_SILU) {
-        // the fast division gives 0 for denominators beyond 2^126, which is the limit here
         const float p = act_sigmoid(g);
         a = g * p;
-        s = p * (1.0f + g * (1.0f - p));
+        s = fmaf(a, 1.0f - p, p);
     } else if (ACT == SCALECOM_ACT_GELU) {
         const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
         a = g * c;
-        s = c + g * __expf(-0.5f * g * g) * 0.39894228040143268f;
+        s = fmaf(g * 0.39894228040143268f, fast_exp2((-0.5f * LOG2_E) * g * g), c);
     } else if (ACT == SCALECOM_ACT_GELU_TANH) {
         if (fabsf(g) > 30.0f) {                 // tanh is +-1 there; the cube below could overflow
             a = g > 0.0f ? g : 0.0f;
@@ -383,6 +426,21 @@ __device__ __forceinline__ uint32_t ring_next(Ring& r) {
     __syncwarp();
     return r.base + uint32_t(r.n++ & (SLOTS - 1)) * (TC_RING / SLOTS);
 }
+// a staged block to global memory, element by element: rows off the 16-byte grid. The whole warp, after a __syncwarp.
+template <int BYTES>
+__device__ __forceinline__ void ring_copy(const TcJob& J, int k, uint32_t slot, int row0, int col0, int plane, int batch) {
+    const TcOut& o = J.out[k];
+    const uint32_t lane = lane_id();
+    const int rows = min(32, J.m - row0);
+    const int64_t at = int64_t(batch) * o.batch + int64_t(plane) * o.plane + int64_t(row0) * o.ld + col0 + lane;
+    if (col0 + int(lane) < J.n) {
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            if (BYTES == 2) reinterpret_cast<uint16_t*>(o.base)[at + r * o.ld] = lds16(slot + piece16(r, lane >> 3) + (lane & 7u) * 2);
+            else reinterpret_cast<uint32_t*>(o.base)[at + r * o.ld] = lds32(slot + piece32(r, lane >> 2) + (lane & 3u) * 4);
+        }
+    }
+}
 // a staged block to global memory at (row0, col0)
 template <int BYTES>
 __device__ __forceinline__ void ring_send(const TcJob& J, int k, uint32_t slot, int row0, int col0, int plane, int batch) {
@@ -396,18 +454,9 @@ __device__ __forceinline__ void ring_send(const TcJob& J, int k, uint32_t slot, 
         }
     } else {
         __syncwarp();
-        const uint32_t lane = lane_id();
-        const int rows = min(32, J.m - row0);
-        const int64_t at = int64_t(batch) * o.batch + int64_t(plane) * o.plane + int64_t(row0) * o.ld + col0 + lane;
-        if (col0 + int(lane) < J.n) {
-#pragma unroll 4
-            for (int r = 0; r < rows; ++r) {
-                if (BYTES == 2) reinterpret_cast<uint16_t*>(o.base)[at + r * o.ld] = lds16(slot + piece16(r, lane >> 3) + (lane & 7u) * 2);
-                else reinterpret_cast<uint32_t*>(o.base)[at + r * o.ld] = lds32(slot + piece32(r, lane >> 2) + (lane & 3u) * 4);
-            }
-        }
+        ring_copy<BYTES>(J, k, slot, row0, col0, plane, batch);
         __syncwarp();
-        if (lane == 0) bulk_commit();               // an empty group: the ring counts one for each block
+        if (lane_id() == 0) bulk_commit();          // an empty group: the ring counts one for each block
     }
 }
 __device__ __forceinline__ uint32_t pack16(int type, float a, float b) {
@@ -430,6 +479,27 @@ __device__ __forceinline__ void stage16(uint32_t slot, int type, const float (&v
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) sts128(slot + piece16(lane, i), p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
+}
+// three 16-bit blocks of one place: x to plane px of output kx, and so on; kx < 0: not wanted
+__device__ __forceinline__ void emit3(const TcJob& J, uint32_t ring, int type, int row0, int col0, int kx, int px, const float (&x)[32], int ky, int py,
+                                      const float (&y)[32], int kz, int pz, const float (&z)[32]) {
+    if (lane_id() == 0) bulk_wait_read<0>();        // the blocks of the place before are on their way
+    __syncwarp();
+    if (kx >= 0) stage16(ring, type, x);
+    if (ky >= 0) stage16(ring + 2048u, type, y);
+    stage16(ring + 4096u, type, z);
+    fence_async_smem();
+    __syncwarp();
+    const bool copy_x = kx >= 0 && !J.out[kx].tma, copy_y = ky >= 0 && !J.out[ky].tma, copy_z = !J.out[kz].tma;
+    if (lane_id() == 0) {
+        if (kx >= 0 && !copy_x) tma_store(&J.o[kx], col0, row0, px, 0, ring);
+        if (ky >= 0 && !copy_y) tma_store(&J.o[ky], col0, row0, py, 0, ring + 2048u);
+        if (!copy_z) tma_store(&J.o[kz], col0, row0, pz, 0, ring + 4096u);
+        bulk_commit();
+    }
+    if (copy_x) ring_copy<2>(J, kx, ring, row0, col0, px, 0);
+    if (copy_y) ring_copy<2>(J, ky, ring + 2048u, row0, col0, py, 0);
+    if (copy_z) ring_copy<2>(J, kz, ring + 4096u, row0, col0, pz, 0);
 }
 template <bool MAY_F32>
 __device__ __forceinline__ void emit(const TcJob& J, int k, Ring& ring, int type, const float (&v)[32], int row0, int col0, int plane, int batch) {
@@ -543,17 +613,25 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
         for (int i = 0; i < 32; ++i) v[i] *= un;
         emit<true>(J, 0, ring, J.type, v, row0, col0, 0, u.batch);
     } else if (EPI == EPI_GATE) {
+        if (PL == 2) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) { v[i] *= un; w[i] *= un; }
-        if (J.out[1].base) {
-            emit<PL == 2>(J, 1, ring, J.type, v, row0, col0, 0, 0);
-            emit<PL == 2>(J, 1, ring, J.type, w, row0, col0, 1, 0);
+            for (int i = 0; i < 32; ++i) { v[i] *= un; w[i] *= un; }
         }
-#define SC_CALL(ACT) gate_row<ACT>(v, v, w)
+        const bool save = J.out[1].base != nullptr;
+        float h[32];
+#define SC_CALL(ACT) gate_row<ACT>(v, h, w)
         SC_FOR_ACT(M.act, SC_CALL)
 #undef SC_CALL
-        if (PL == 2) top = max(top, row_top(v, inside ? nc : 0));
-        emit<PL == 2>(J, 0, ring, J.type, v, row0, col0, 0, 0);
+        if (PL == 1) {
+            emit3(J, ring.base, J.type, row0, col0, save ? 1 : -1, 0, v, save ? 1 : -1, 1, w, 0, 0, h);
+        } else {
+            if (save) {
+                emit<true>(J, 1, ring, J.type, v, row0, col0, 0, 0);
+                emit<true>(J, 1, ring, J.type, w, row0, col0, 1, 0);
+            }
+            top = max(top, row_top(h, inside ? nc : 0));
+            emit<true>(J, 0, ring, J.type, h, row0, col0, 0, 0);
+        }
     } else if (EPI == EPI_GATE_BWD) {
         float g[32];
         if (PL == 1 && M.in_tma) {
@@ -569,8 +647,10 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
             load_typed(J.type, M.in, at, g, inside ? nc : 0);
             load_typed(J.type, M.in, at + M.in_plane, w, inside ? nc : 0);
         }
+        if (PL == 2) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= un;
+            for (int i = 0; i < 32; ++i) v[i] *= un;
+        }
 #define SC_CALL(ACT) gate_back_row<ACT>(g, v, w)
         SC_FOR_ACT(M.act, SC_CALL)
 #undef SC_CALL
@@ -578,9 +658,13 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
             top = max(top, max(row_top(g, inside ? nc : 0), row_top(w, inside ? nc : 0)));
             top2 = max(top2, row_top(v, inside ? nc : 0));
         }
-        emit<PL == 2>(J, 0, ring, J.type, g, row0, col0, 0, 0);
-        emit<PL == 2>(J, 0, ring, J.type, w, row0, col0, 1, 0);
-        emit<PL == 2>(J, 0, ring, J.type, v, row0, col0, 2, 0);
+        if (PL == 1) {
+            emit3(J, ring.base, J.type, row0, col0, 0, 0, g, 0, 1, w, 0, 2, v);
+        } else {
+            emit<true>(J, 0, ring, J.type, g, row0, col0, 0, 0);
+            emit<true>(J, 0, ring, J.type, w, row0, col0, 1, 0);
+            emit<true>(J, 0, ring, J.type, v, row0, col0, 2, 0);
+        }
     } else if (EPI == EPI_PLANES) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= J.alpha;
@@ -647,6 +731,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
         abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 3 && lane < 2u * uint32_t(NJ)) {                 // the operands' tensor maps are fetched while the rest is set up
+        asm volatile("prefetch.tensormap [%0];" ::"l"(lane & 1u ? &P.job[lane / 2].b[0] : &P.job[lane / 2].a[0]) : "memory");
     }
     if (warp == 2) {
         if (CG == 2) {
@@ -768,8 +855,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
         uint32_t top = 0u, top2 = 0u;
         int n_acc = 0;
         const uint32_t stage0 = tiles0 + S::STAGES * S::STAGE_BYTES;
-        Ring ring = {stage0 + (warp - 4u) * TC_RING, 0};
-        Inflow in = {stage0 + TC_EPI_WARPS * TC_RING + (warp - 4u) * S::IN_BYTES, inflow0 + 8u * (warp - 4u), 0u, false};
+        Ring ring = {stage0 + (warp - 4u) * S::RING, 0};
+        Inflow in = {stage0 + TC_EPI_WARPS * S::RING + (warp - 4u) * S::IN_BYTES, inflow0 + 8u * (warp - 4u), 0u, false};
         auto begin = [&](const TcUnit& u, int row0, int c) {
             if (S::LOADS && c < CHUNKS) inflow_start<EPI>(P.job[NJ > 1 ? u.job : 0], P.more, in, row0, u.nt * WIDTH + chunk(c), u.batch);
         };
@@ -781,7 +868,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             if (J.amax_a) un_scale *= plane_unscale(*J.amax_a) * plane_unscale(*J.amax_b);
             const int row0 = u.mt * S::BM + int(rank) * TC_BM + int(quad) * 32;
             float v[32], w[32];
-            float sum[PL == 2 ? BN / 64 : 1][32];       // PL = 2: this thread's columns, in the order of `column`
+            float sum[BN / 64][32];       // PL = 2: this thread's columns, in the order of `column`
             auto column = [&](int c) {                  // TMEM column of the thread's c-th 32 columns
                 if (EPI == EPI_GATE && PL == 2) return (c & 1) * (BN / 2) + (int(half) * (BN / 128) + (c >> 1)) * 32;
                 return int(half) * (BN / 2) + c * 32;
@@ -803,10 +890,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     tc_fence_after();
                     acc = tmem + q * BN + lanes;
 #pragma unroll
-                    for (int c = 0; c < BN / 64; ++c) {
-                        tc_ld32(acc + column(c), v);
+                    for (int c = 0; c < BN / 64; c += 2) {
+                        tc_ld32x2(acc + column(c), v, acc + column(c + 1), w);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) sum[c][i] += v[i];
+                        for (int i = 0; i < 32; ++i) {
+                            sum[c][i] += v[i];
+                            sum[c + 1][i] += w[i];
+                        }
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -878,8 +968,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
 #pragma unroll 1
                 for (int c = 0; c < CHUNKS; ++c) {
                     const int at = chunk(c);
-                    tc_ld32(acc + at, v);
-                    if (EPI == EPI_GATE) tc_ld32(acc + BN / 2 + at, w);
+                    if (EPI == EPI_GATE) tc_ld32x2(acc + at, v, acc + BN / 2 + at, w);
+                    else tc_ld32(acc + at, v);
                     if (c == CHUNKS - 1) release();
                     if (ok) begin(u, row0, c);
                     ok = ok && tc_epilogue<EPI, PL>(J, P.more, u, row0, u.nt * WIDTH + at, c + 1 < CHUNKS ? u.nt * WIDTH + chunk(c + 1) : -1, v, w, un_scale,
@@ -889,7 +979,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
         }
         if (lane == 0) {
             if (in.pending) mbar_drain(in.bar, in.phase);
-            bulk_wait_all();                        // the staging area is read, and the results are written, before the block ends
+            bulk_wait_read<0>();                    // the staging area is read before the block ends; the writes end with the kernel
         }
         if (PL == 2 && (EPI == EPI_GATE || EPI == EPI_GATE_BWD)) {
             if (P.more.amax_o) {
