@@ -391,8 +391,8 @@ __device__ __forceinline__ TcUnit tc_unit(const TcParams<NJ>& P, int u) {
         }
         r.mt = mt;
         r.nt = t;
-    } else {                                      // bands of 2048 rows, column by column: the band's A stays in L2
-        constexpr int BAND = 2048 / BM;
+    } else {                                      // bands of 4096 rows, column by column: the band's A stays in L2
+        constexpr int BAND = 4096 / BM;
         const int band = t / (BAND * J.nt), first = band * BAND;
         const int rows = J.mt - first < BAND ? J.mt - first : BAND;
         const int in = t - band * BAND * J.nt;
