@@ -95,7 +95,7 @@ int scalecom_layer_norm(scalecom_ops* ops, int32_t dtype, int64_t rows, int64_t 
  *   gamma       NULL: ones.      dx  may be dy itself (same row distance); NULL if not wanted.
  *   dgamma, dbeta  DEVICE fp32[width], written (not added to); NULL (each) if not wanted.
  * rows = 0: dgamma and dbeta are filled with zeros.
- * Scratch: 32 * width bytes for each multiprocessor.
+ * Scratch: 32 * width bytes for each multiprocessor (rows longer than 8192 elements: 2 KB * multiprocessors * 8 + 8 * width in all).
  */
 int scalecom_layer_norm_backward(scalecom_ops* ops, int32_t dtype, int64_t rows, int64_t width,
                                  const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* gamma,

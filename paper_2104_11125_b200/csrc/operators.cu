@@ -149,6 +149,11 @@ cudaError_t ln_forward_t(scalecom_ops* o, const LnParams& P) {
     return vec ? ln_forward<T, V>(o, P) : ln_forward<T, 1>(o, P);
 }
 
+// rows longer than this leave the registers
+constexpr int LN_MOST_WIDTH = 8192;
+// blocks to a column of the long rows' column sums
+int64_t ln_wide_groups(const scalecom_ops* o, int64_t width) { return ceil_div(int64_t(o->sms) * 8, ceil_div(width, LN_THREADS)); }
+
 template <typename T, int VEC, int NV, int TPR, bool DW>
 cudaError_t ln_launch_backward_dw(scalecom_ops* o, LnParams& P) {
     const auto kernel = layer_norm_backward_kernel<T, VEC, NV, TPR, DW>;
@@ -185,9 +190,8 @@ cudaError_t ln_backward(scalecom_ops* o, LnParams& P) {
     if (VEC == 1 && w <= 32 * B) return ln_launch_backward<T, VEC, VEC == 1 ? 32 : 1, LN_THREADS>(o, P);
     if (P.dgamma || P.dbeta) {                            // before dx, which may overwrite dy
         const int64_t cols = ceil_div(w, LN_THREADS);
-        int64_t groups = ceil_div(int64_t(o->sms) * 8, cols);
+        int64_t groups = ln_wide_groups(o, w);
         if (groups > P.rows) groups = P.rows;
-        if (groups > o->sms * LN_MOST_BLOCKS) groups = o->sms * LN_MOST_BLOCKS;
         P.nblocks = int32_t(groups);
         const cudaError_t e = launch(o, layer_norm_columns_kernel<T>, dim3(unsigned(cols), unsigned(groups)), LN_THREADS, 0, P);
         if (e != cudaSuccess) return e;
@@ -1058,7 +1062,7 @@ int scalecom_layer_norm_backward(scalecom_ops* o, int32_t dtype, int64_t rows, i
     if (!dx && !dgamma && !dbeta) return SCALECOM_OK;
     const bool dw = dgamma || dbeta;
     if (dw) {
-        rc = ensure_ws(o, size_t(o->sms) * LN_MOST_BLOCKS * 2 * size_t(width) * 4);
+        rc = ensure_ws(o, size_t(width > LN_MOST_WIDTH ? ln_wide_groups(o, width) : int64_t(o->sms) * LN_MOST_BLOCKS) * 2 * size_t(width) * 4);
         if (rc != SCALECOM_OK) return rc;
     }
     LnParams P;

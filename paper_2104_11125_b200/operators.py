@@ -67,22 +67,23 @@ def _type(t: torch.Tensor, name: str) -> int:
     return kind
 
 
-def _matrix(t: torch.Tensor, kind: torch.dtype, rows: int, cols: int, name: str) -> int:
+def _matrix(t: torch.Tensor, kind: torch.dtype, shape: torch.Size, name: str) -> int:
     """Row distance of a matrix whose rows are contiguous (a slice of longer rows is fine)."""
-    if not t.is_cuda or t.dtype != kind:
+    if t.dtype is not kind or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor of %s" % (name, kind))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError("%s must be %d x %d" % (name, rows, cols))
+    if t.shape != shape or len(shape) != 2:
+        raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
     s0, s1 = t.stride()
-    if (cols > 1 and s1 != 1) or (rows > 1 and s0 < cols):
+    rows, cols = shape
+    if (s1 != 1 and cols > 1) or (s0 < cols and rows > 1):
         raise ValueError("%s must have contiguous rows" % name)
-    return s0 if rows > 1 else max(s0, cols)
+    return s0 if s0 >= cols else cols
 
 
 def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n):
+    if not (t.is_cuda and t.dtype is torch.float32 and t.numel() == n and t.is_contiguous()):
         raise TypeError("%s must be a contiguous CUDA float32 tensor of %d elements" % (name, n))
     return t.data_ptr()
 
@@ -90,9 +91,9 @@ def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
 def _whole(t: Optional[torch.Tensor], kinds: Sequence[torch.dtype], shape, name: str) -> Optional[int]:
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype in kinds and t.is_contiguous()):
+    if t.dtype not in kinds or not t.is_cuda or not t.is_contiguous():
         raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, " or ".join(map(str, kinds))))
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError("%s must be of shape %s" % (name, shape))
     return t.data_ptr()
 
@@ -101,9 +102,13 @@ class Operators:
     """One operator handle: a stream binding and scratch.  Inputs and outputs belong to the caller."""
 
     def __init__(self, stream: Optional[torch.cuda.Stream] = None):
-        h = ctypes.c_void_p()
-        _check(lib().scalecom_ops_create(ctypes.byref(h)), "scalecom_ops_create")
+        h, L = ctypes.c_void_p(), lib()
+        _check(L.scalecom_ops_create(ctypes.byref(h)), "scalecom_ops_create")
         self._h = h.value
+        # looked up once: a small call's time is its way through here
+        self._layer_norm, self._layer_norm_backward = L.scalecom_layer_norm, L.scalecom_layer_norm_backward
+        self._gated_ffn, self._gated_ffn_backward = L.scalecom_gated_ffn, L.scalecom_gated_ffn_backward
+        self._orthogonalise = L.scalecom_orthogonalise
         if stream is not None:
             self.set_stream(stream)
 
@@ -142,35 +147,38 @@ class Operators:
     def layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,
                    mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None) -> None:
         """y = (x - mean) * rstd * gamma + beta over the last dimension of the matrix x."""
-        kind = _type(x, "x")
-        rows, width = x.shape
-        _check(lib().scalecom_layer_norm(self._h, kind, rows, width, x.data_ptr(), _matrix(x, x.dtype, rows, width, "x"),
+        kind, shape = x.dtype, x.shape
+        code = _type(x, "x")
+        rows, width = shape
+        _check(self._layer_norm(self._h, code, rows, width, x.data_ptr(), _matrix(x, kind, shape, "x"),
                                          _vector(gamma, width, "gamma"), _vector(beta, width, "beta"), eps,
-                                         y.data_ptr(), _matrix(y, x.dtype, rows, width, "y"),
+                                         y.data_ptr(), _matrix(y, kind, shape, "y"),
                                          _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd")), "scalecom_layer_norm")
 
     def layer_norm_backward(self, dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
                             dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
                             dbeta: Optional[torch.Tensor] = None) -> None:
         """dx, and the gradients of gamma and beta (written, not added to)."""
-        kind = _type(x, "x")
-        rows, width = x.shape
-        _check(lib().scalecom_layer_norm_backward(
-            self._h, kind, rows, width, dy.data_ptr(), _matrix(dy, x.dtype, rows, width, "dy"),
-            x.data_ptr(), _matrix(x, x.dtype, rows, width, "x"), _vector(gamma, width, "gamma"),
+        kind, shape = x.dtype, x.shape
+        code = _type(x, "x")
+        rows, width = shape
+        _check(self._layer_norm_backward(
+            self._h, code, rows, width, dy.data_ptr(), _matrix(dy, kind, shape, "dy"),
+            x.data_ptr(), _matrix(x, kind, shape, "x"), _vector(gamma, width, "gamma"),
             _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
-            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dx, x.dtype, rows, width, "dx"),
+            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dx, kind, shape, "dx"),
             _vector(dgamma, width, "dgamma"), _vector(dbeta, width, "dbeta")), "scalecom_layer_norm_backward")
 
     def gated_ffn(self, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, y: torch.Tensor,
                   saved: Optional[torch.Tensor] = None, activation: str = "silu") -> None:
         """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; saved [2, tokens, hidden] keeps what the backward pass needs."""
-        kind = _type(x, "x")
-        (tokens, width), hidden, k = x.shape, w_gate.shape[0], (x.dtype,)
-        _check(lib().scalecom_gated_ffn(
-            self._h, kind, ACTIVATIONS[activation], tokens, width, hidden, x.data_ptr(), _matrix(x, x.dtype, tokens, width, "x"),
+        kind, shape = x.dtype, x.shape
+        code = _type(x, "x")
+        (tokens, width), hidden, k = shape, w_gate.shape[0], (kind,)
+        _check(self._gated_ffn(
+            self._h, code, ACTIVATIONS[activation], tokens, width, hidden, x.data_ptr(), _matrix(x, kind, shape, "x"),
             _whole(w_gate, k, (hidden, width), "w_gate"), _whole(w_up, k, (hidden, width), "w_up"),
-            _whole(w_down, k, (width, hidden), "w_down"), y.data_ptr(), _matrix(y, x.dtype, tokens, width, "y"),
+            _whole(w_down, k, (width, hidden), "w_down"), y.data_ptr(), _matrix(y, kind, shape, "y"),
             _whole(saved, k, (2, tokens, hidden), "saved")), "scalecom_gated_ffn")
 
     def gated_ffn_backward(self, dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
@@ -178,18 +186,19 @@ class Operators:
                            dw_up: Optional[torch.Tensor] = None, dw_down: Optional[torch.Tensor] = None,
                            activation: str = "silu") -> None:
         """Gradients of the block (written, not added to); the weights' may be float32 whatever the type of x."""
-        kind = _type(x, "x")
-        (tokens, width), hidden, k = x.shape, w_gate.shape[0], (x.dtype,)
+        kind, shape = x.dtype, x.shape
+        code = _type(x, "x")
+        (tokens, width), hidden, k = shape, w_gate.shape[0], (kind,)
         grads = [g for g in (dw_gate, dw_up, dw_down) if g is not None]
-        gk = (grads[0].dtype if grads else x.dtype,)
-        if gk[0] not in (x.dtype, torch.float32):
+        gk = (grads[0].dtype if grads else kind,)
+        if gk[0] not in (kind, torch.float32):
             raise TypeError("weight gradients must be of x's type or float32")
-        _check(lib().scalecom_gated_ffn_backward(
-            self._h, kind, TYPES[gk[0]], ACTIVATIONS[activation], tokens, width, hidden,
-            dy.data_ptr(), _matrix(dy, x.dtype, tokens, width, "dy"), x.data_ptr(), _matrix(x, x.dtype, tokens, width, "x"),
+        _check(self._gated_ffn_backward(
+            self._h, code, TYPES[gk[0]], ACTIVATIONS[activation], tokens, width, hidden,
+            dy.data_ptr(), _matrix(dy, kind, shape, "dy"), x.data_ptr(), _matrix(x, kind, shape, "x"),
             _whole(w_gate, k, (hidden, width), "w_gate"), _whole(w_up, k, (hidden, width), "w_up"),
             _whole(w_down, k, (width, hidden), "w_down"), _whole(saved, k, (2, tokens, hidden), "saved"),
-            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dx, x.dtype, tokens, width, "dx"),
+            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dx, kind, shape, "dx"),
             _whole(dw_gate, gk, (hidden, width), "dw_gate"), _whole(dw_up, gk, (hidden, width), "dw_up"),
             _whole(dw_down, gk, (width, hidden), "dw_down")), "scalecom_gated_ffn_backward")
 
@@ -213,6 +222,6 @@ class Operators:
         if len(flat) not in (3, 3 * steps):
             raise ValueError("coefficients must be one triple, or one for each step")
         co = (ctypes.c_float * len(flat))(*flat)
-        _check(lib().scalecom_orthogonalise(self._h, batch, rows, cols, kin, update.data_ptr(), ld[0], stride[0], kout, out.data_ptr(),
+        _check(self._orthogonalise(self._h, batch, rows, cols, kin, update.data_ptr(), ld[0], stride[0], kout, out.data_ptr(),
                                             ld[1], stride[1], int(steps), ctypes.cast(co, ctypes.c_void_p), len(flat) // 3, eps, scale),
                "scalecom_orthogonalise")
