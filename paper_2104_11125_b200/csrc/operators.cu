@@ -291,15 +291,15 @@ struct Product {
 struct Plan { int bn, cg, splits; int64_t mt, nt, tiles; };
 
 // Tile shape and parts of k: the least estimated time. A tile's 64 k take the tensor core (256 cycles for 128 columns, three
-// times that for two planes, of which 1,900 cycles become with the sums in registers) or the 53 bytes a clock that an SM was
+// times that for two planes, which with the sums in registers become 1,900 cycles for 128 columns and some 2,600 for 256) or the 53 bytes a clock that an SM was
 // seen to get from L2, whichever is longer; what a tile adds at its end is only
 // seen once, behind the last wave; parts of k cost fences and counting (about 6,000 cycles) and their accumulators' way through L2.
 Plan make_plan(const scalecom_ops* o, int epi, int planes, int64_t m, int64_t n, int64_t iters, int64_t batch) {
     struct Shape { int bn, cg; };
-    static const Shape one[] = {{256, 2}, {128, 2}, {128, 1}}, two[] = {{128, 2}, {128, 1}};
+    static const Shape one[] = {{256, 2}, {128, 2}, {128, 1}}, two[] = {{256, 2}, {128, 2}, {128, 1}};
     Plan best = {};
     double least = 1e300;
-    for (int i = 0; i < (planes > 1 ? 2 : 3); ++i) {
+    for (int i = 0; i < 3; ++i) {
         const Shape t = planes > 1 ? two[i] : one[i];
         const int bm = TC_BM * t.cg;
         Plan p;
@@ -316,7 +316,7 @@ Plan make_plan(const scalecom_ops* o, int epi, int planes, int64_t m, int64_t n,
             }
         }
         const double math = t.bn * 2.0 * (planes > 1 ? 3.0 : 1.0), bytes = planes * (16384.0 + t.bn / t.cg * 128.0);
-        const double block = planes > 1 ? 1900.0 : math > bytes / 53.0 ? math : bytes / 53.0, drain = t.bn * 12.0;
+        const double block = planes > 1 ? (t.bn == 256 ? 2600.0 : 1900.0) : math > bytes / 53.0 ? math : bytes / 53.0, drain = t.bn * 12.0;
         for (int s = 1; s <= 32 && (s == 1 || s * 2 <= iters); ++s) {
             if (s > 1 && p.tiles * batch * t.cg > MAX_SPLIT_TILES) break;
             const double waves = double(ceil_div(p.tiles * batch * s, o->sms / t.cg));
@@ -345,7 +345,7 @@ cudaError_t tc_launch(scalecom_ops* o, const TcParams<NJ>& P) {
 }
 template <int EPI>
 cudaError_t tc_launch_any(scalecom_ops* o, const Plan& pl, int planes, const TcParams<1>& P) {
-    if (planes > 1) return pl.cg == 2 ? tc_launch<128, EPI, 2, 2>(o, P) : tc_launch<128, EPI, 2, 1>(o, P);
+    if (planes > 1) return pl.bn == 256 ? tc_launch<256, EPI, 2, 2>(o, P) : pl.cg == 2 ? tc_launch<128, EPI, 2, 2>(o, P) : tc_launch<128, EPI, 2, 1>(o, P);
     if (pl.cg == 1) return tc_launch<128, EPI, 1, 1>(o, P);
     return pl.bn == 256 ? tc_launch<256, EPI, 1, 2>(o, P) : tc_launch<128, EPI, 1, 2>(o, P);
 }
@@ -358,6 +358,7 @@ cudaError_t tc_attributes() {
     cudaError_t e = tc_attribute<256, EPI, 1, 2>();
     if (e == cudaSuccess) e = tc_attribute<128, EPI, 1, 2>();
     if (e == cudaSuccess) e = tc_attribute<128, EPI, 1, 1>();
+    if (e == cudaSuccess) e = tc_attribute<256, EPI, 2, 2>();
     if (e == cudaSuccess) e = tc_attribute<128, EPI, 2, 2>();
     if (e == cudaSuccess) e = tc_attribute<128, EPI, 2, 1>();
     return e;
@@ -432,15 +433,20 @@ int run_stores(scalecom_ops* o, const Stored* list, int n, float* partial) {
     const int planes = list[0].p->a->planes;
     Plan pl[TC_JOBS];
     int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) {
-        const Product& p = *list[i].p;
-        pl[i].bn = planes > 1 ? 128 : 256;
-        pl[i].cg = 2;
-        pl[i].splits = 1;
-        pl[i].mt = ceil_div(p.m, 2 * TC_BM);
-        pl[i].nt = ceil_div(p.n, pl[i].bn);
-        pl[i].tiles = pl[i].mt * pl[i].nt;
-        tiles += pl[i].tiles;
+    int bn = 256;
+    for (; bn >= (planes > 1 ? 128 : 256); bn /= 2) {        // with two planes the narrow tiles cost little more
+        tiles = 0;
+        for (int i = 0; i < n; ++i) {
+            const Product& p = *list[i].p;
+            pl[i].bn = bn;
+            pl[i].cg = 2;
+            pl[i].splits = 1;
+            pl[i].mt = ceil_div(p.m, 2 * TC_BM);
+            pl[i].nt = ceil_div(p.n, bn);
+            pl[i].tiles = pl[i].mt * pl[i].nt;
+            tiles += pl[i].tiles;
+        }
+        if (tiles >= o->sms / 2) break;
     }
     if (n > 1 && tiles >= o->sms / 2) {
         TcParams<TC_JOBS> P;
@@ -455,7 +461,8 @@ int run_stores(scalecom_ops* o, const Stored* list, int n, float* partial) {
         }
         P.jobs = n;
         P.status = o->ctrl;
-        const cudaError_t e = planes > 1 ? tc_launch<128, EPI_STORE, 2, 2>(o, P) : tc_launch<256, EPI_STORE, 1, 2>(o, P);
+        const cudaError_t e = planes == 1 ? tc_launch<256, EPI_STORE, 1, 2>(o, P) : bn == 256 ? tc_launch<256, EPI_STORE, 2, 2>(o, P)
+                                                                                             : tc_launch<128, EPI_STORE, 2, 2>(o, P);
         if (e == cudaSuccess) return SCALECOM_OK;
         cudaGetLastError();
         return SCALECOM_ERR_CUDA;
@@ -751,7 +758,7 @@ int small_cluster(const scalecom_ops* o, int planes, int64_t r, int64_t n, int64
         if (nss_smem(planes, rp, nc, c) > 225 * 1024) continue;
         const double waves = double(ceil_div(batch * c, o->sms));
         const double mma = 2.0 * (tiles * (nc / 16) + tiles * side + (nc / 16) * side * side) * (planes > 1 ? 3 : 1);
-        const double cost = waves * (steps * (mma * 20.0 / 4.0 + 1500.0 + (c > 1 ? 7000.0 + 1500.0 * ceil_div(tiles, NSS_WARPS) * ceil_div(c, 4) : 0.0)) + 4000.0 + double(rp) * nc / 16.0);
+        const double cost = waves * (steps * (mma * 20.0 / 4.0 + 1500.0 + (c > 1 ? (planes > 1 ? 12000.0 : 4000.0) + 1500.0 * ceil_div(tiles, NSS_WARPS) * ceil_div(c, 4) : 0.0)) + 4000.0 + double(rp) * nc / 16.0);
         if (cost < least * 0.95) {
             least = cost;
             best = c;
@@ -931,6 +938,7 @@ int scalecom_ops_create(scalecom_ops** out) {
     }
     if (e == cudaSuccess) e = tc_attributes<EPI_STORE>();
     if (e == cudaSuccess) e = tc_attribute<256, EPI_STORE, 1, 2, TC_JOBS>();
+    if (e == cudaSuccess) e = tc_attribute<256, EPI_STORE, 2, 2, TC_JOBS>();
     if (e == cudaSuccess) e = tc_attribute<128, EPI_STORE, 2, 2, TC_JOBS>();
     if (e == cudaSuccess) e = tc_attributes<EPI_GATE>();
     if (e == cudaSuccess) e = tc_attributes<EPI_GATE_BWD>();

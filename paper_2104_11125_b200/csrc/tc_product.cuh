@@ -21,8 +21,8 @@
 // PL = 2, for fp32 values: each operand is two fp16 planes, x = hi + lo, and a block of k contributes lo hi + hi lo + hi hi.
 // The tensor core truncates its fp32 accumulator after every 16 k (measured: 2.2e-8 of the result for each, always towards
 // zero, so 2048 k are 3e-6 low), which is why the accumulator is not kept there: after each 64 k, small products first, the epilogue
-// warps add it to sums in registers with correct rounding.  Three accumulators in turn cover the way from the tensor core to those warps
-// and back; the finished sums go to the fourth quarter of TMEM, from where the epilogue proceeds as with one plane.
+// warps add it to sums in registers with correct rounding.  Two to four accumulators in turn cover the way from the tensor core to
+// those warps and back; the finished sums go to the place of the last one, from where the epilogue proceeds as with one plane.
 #pragma once
 #include <cuda.h>
 
@@ -56,8 +56,9 @@ template <int BN, int EPI, int PL, int CG> struct TcShape {
     static constexpr int STAGES = (227 * 1024 - 1024 - 512 - EPI_BYTES) / STAGE_BYTES;
     static constexpr int BM = TC_BM * CG;                            // rows of a tile
     static constexpr int SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 1024;         // + alignment of the swizzle atoms
-    static constexpr int ACCS = PL == 2 ? 3 : 2;                     // accumulators in TMEM
-    static constexpr int TMEM_COLS = PL == 2 ? 4 * BN : 2 * BN;      // PL = 2: and the sums
+    static constexpr int ACCS = PL == 2 ? 512 / BN : 2;              // accumulators in TMEM
+    static constexpr int TMEM_COLS = ACCS * BN;
+    static constexpr bool MANY_REGS = PL == 2 && BN == 256;          // 128 sums a thread: the epilogue warps take registers from the others
 };
 
 enum TcEpilogue { EPI_STORE = 0, EPI_GATE = 1, EPI_GATE_BWD = 2, EPI_GRAM = 3, EPI_POLY = 4, EPI_PLANES = 5 };
@@ -757,6 +758,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
     const int units = tc_units(P);
     const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
+    // 384 threads x 168 registers at launch = 128 x 56 + 256 x 224
+    if (warp < 4) {
+    if (S::MANY_REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0) {
         if (lane == 0) {
             int n_issued = 0;                       // copies issued so far; stage and phase follow from it
@@ -841,7 +845,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 mbar_drain(drain, 0);
             }
         }
-    } else if (warp >= 4) {
+    }
+    } else {
+        if (S::MANY_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2;
         const uint32_t lanes = (quad * 32u) << 16;
         const int tid = int(threadIdx.x) - 128;
@@ -898,13 +904,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                             sum[c + 1][i] += w[i];
                         }
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) acc_free(q);
+                    if (it + TC_CHUNK < it1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) acc_free(q);
+                    }
                 }
-                acc = tmem + S::ACCS * BN + lanes;
+                // the last accumulator is kept until the epilogue has read the sums from its place
 #pragma unroll
-                for (int c = 0; c < BN / 64; ++c) tc_st32(acc + column(c), sum[c]);
+                for (int c = 0; c < BN / 64; ++c)
+                    if (ok) tc_st32(acc + column(c), sum[c]);
                 tc_wait_st();
             } else {
                 q = n_acc % S::ACCS;
@@ -916,11 +925,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             if (!ok) break;
             tc_fence_after();
             auto release = [&]() {                          // the accumulator is free once its last columns are in registers
-                if (PL == 1) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) acc_free(q);
-                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) acc_free(q);
             };
             if (J.splits > 1) {
                 // this part's accumulators to scratch, [column][row]; the block that arrives last adds the parts up in their order
