@@ -96,11 +96,14 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float2 (*part)[LN_T
 
 // A thread's columns of a row as they lie in memory, loaded ahead of their use.
 template <typename T, int VEC, int NV> struct LnRow { Pack<T, VEC> p[NV]; };
-template <typename T, int VEC, int NV, int TPR>
-__device__ __forceinline__ void ln_fetch(const T* row, int t, int width, LnRow<T, VEC, NV>& r) {
+// MOST: the row reaches into the last of the thread's NV places, so only that one is compared with the width (a limit
+// no column reaches stands for the others, and the comparisons are dropped).
+constexpr int LN_NO_LIMIT = 1 << 30;
+template <typename T, int VEC, int NV, int TPR, bool MOST>
+__device__ __forceinline__ void ln_fetch(const T* row, int t, int row_width, LnRow<T, VEC, NV>& r) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int col = (i * TPR + t) * VEC;
+        const int col = (i * TPR + t) * VEC, width = MOST && i + 1 < NV ? LN_NO_LIMIT : row_width;
         if (col + VEC <= width) {
             r.p[i] = *reinterpret_cast<const Pack<T, VEC>*>(row + col);
         } else {
@@ -144,7 +147,7 @@ __device__ __forceinline__ void ln_store(T* p, int col, int width, const float (
 // WHOLE: the row fills the threads' columns exactly; its moments take one barrier and no comparisons of columns with the width.
 // The 16384 x 4096 bf16 case is as close to the issue rate as to HBM: with values converted three times, comparisons and
 // quotients in the joins it took 128 us.
-template <typename T, int VEC, int NV, int TPR, bool WHOLE>
+template <typename T, int VEC, int NV, int TPR, bool WHOLE, bool MOST>
 __global__ void __launch_bounds__(LN_THREADS, ln_blocks(3 * NV * VEC + 2 * NV * VEC * int(sizeof(T)) / 4 + 16)) layer_norm_kernel(const LnParams P) {
     __shared__ float2 part[2][LN_THREADS / 32];
     constexpr int RPB = LN_THREADS / TPR;
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(LN_THREADS, ln_blocks(3 * NV * VEC + 2 * NV * 
     chain_wait();
     LnRow<T, VEC, NV> next, after;
     auto fetch = [&](int64_t r, LnRow<T, VEC, NV>& to) {
-        if (r < P.rows) ln_fetch<T, VEC, NV, TPR>(static_cast<const T*>(P.x) + r * P.ldx, t, width, to);
+        if (r < P.rows) ln_fetch<T, VEC, NV, TPR, MOST>(static_cast<const T*>(P.x) + r * P.ldx, t, width, to);
     };
     fetch(row, next);
     fetch(row + step, after);
@@ -189,7 +192,7 @@ __global__ void __launch_bounds__(LN_THREADS, ln_blocks(3 * NV * VEC + 2 * NV * 
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
                     const float d = v[i][j] - mean;
-                    m2 += (i * TPR + t) * VEC + j < width ? d * d : 0.0f;
+                    m2 += (MOST && i + 1 < NV) || (i * TPR + t) * VEC + j < width ? d * d : 0.0f;
                 }
             m2 = row_sum<TPR>(m2, &part[1][0].x);
         }
@@ -197,12 +200,12 @@ __global__ void __launch_bounds__(LN_THREADS, ln_blocks(3 * NV * VEC + 2 * NV * 
         T* y = static_cast<T*>(P.y) + row * P.ldy;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int col = (i * TPR + t) * VEC;
-            if (col < width) {
+            const int col = (i * TPR + t) * VEC, limit = MOST && i + 1 < NV ? LN_NO_LIMIT : width;
+            if (col < limit) {
                 float o[VEC];
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) o[j] = (v[i][j] - mean) * rstd * gamma[i][j] + beta[i][j];
-                ln_store<T, VEC>(y, col, width, o);
+                ln_store<T, VEC>(y, col, limit, o);
             }
         }
         if (t == 0) {
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(LN_THREADS) layer_norm_wide_kernel(const LnPar
 
 // Backward. A block walks over rows with a fixed assignment of columns to threads, so each thread keeps its columns' sums for
 // dgamma and dbeta in registers; the blocks' sums go to scratch and a second kernel adds them in block order.
-template <typename T, int VEC, int NV, int TPR, bool DW>
+template <typename T, int VEC, int NV, int TPR, bool DW, bool MOST>
 __global__ void __launch_bounds__(LN_THREADS, ln_blocks(5 * NV * VEC + (NV * VEC <= 16 ? 4 : 2) * NV * VEC * int(sizeof(T)) / 4 + 24)) layer_norm_backward_kernel(const LnParams P) {
     __shared__ float2 part[2][LN_THREADS / 32];
     extern __shared__ float cols[];                       // TPR = 32: [warps][2][width], to join the warps' sums
@@ -276,8 +279,8 @@ __global__ void __launch_bounds__(LN_THREADS, ln_blocks(5 * NV * VEC + (NV * VEC
     float mean = 0.0f, rstd = 0.0f, mean2 = 0.0f, rstd2 = 0.0f;
     auto fetch = [&](int64_t r, LnRow<T, VEC, NV>& a, LnRow<T, VEC, NV>& b, float& mu, float& rs) {
         if (r < P.rows) {
-            ln_fetch<T, VEC, NV, TPR>(static_cast<const T*>(P.x) + r * P.ldx, t, P.width, a);
-            ln_fetch<T, VEC, NV, TPR>(static_cast<const T*>(P.dy) + r * P.lddy, t, P.width, b);
+            ln_fetch<T, VEC, NV, TPR, MOST>(static_cast<const T*>(P.x) + r * P.ldx, t, P.width, a);
+            ln_fetch<T, VEC, NV, TPR, MOST>(static_cast<const T*>(P.dy) + r * P.lddy, t, P.width, b);
             mu = P.mean_in[r];
             rs = P.rstd_in[r];
         }
@@ -293,7 +296,7 @@ __global__ void __launch_bounds__(LN_THREADS, ln_blocks(5 * NV * VEC + (NV * VEC
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const bool in = VEC == 1 || (i * TPR + t) * VEC + j < P.width;
+                const bool in = VEC == 1 || (MOST && i + 1 < NV) || (i * TPR + t) * VEC + j < P.width;
                 xh[i][j] = in ? (pack_get<T, VEC>(x.p[i], j) - mean) * rstd : 0.0f;
                 w[i][j] = pack_get<T, VEC>(dy.p[i], j);      // 0 beyond the row
                 if (DW) {
@@ -310,12 +313,12 @@ __global__ void __launch_bounds__(LN_THREADS, ln_blocks(5 * NV * VEC + (NV * VEC
             T* dx = static_cast<T*>(P.dx) + row * P.lddx;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int col = (i * TPR + t) * VEC;
-                if (col < P.width) {
+                const int col = (i * TPR + t) * VEC, width = MOST && i + 1 < NV ? LN_NO_LIMIT : P.width;
+                if (col < width) {
                     float o[VEC];
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) o[j] = rstd * (w[i][j] - m1 - xh[i][j] * m2);
-                    ln_store<T, VEC>(dx, col, P.width, o);
+                    ln_store<T, VEC>(dx, col, width, o);
                 }
             }
         }

@@ -117,13 +117,16 @@ int64_t resident(const scalecom_ops* o, K kernel, int threads, size_t smem, int 
     return int64_t(o->sms) * per;
 }
 
-template <typename T, int VEC, int NV, int TPR, bool WHOLE = false>
+template <typename T, int VEC, int NV, int TPR, bool WHOLE = false, bool MOST = false>
 cudaError_t ln_launch(scalecom_ops* o, const LnParams& P) {
     if constexpr (!WHOLE && VEC > 1)
-        if (P.width == NV * VEC * TPR) return ln_launch<T, VEC, NV, TPR, true>(o, P);
-    static const int64_t cap = resident(o, layer_norm_kernel<T, VEC, NV, TPR, WHOLE>, LN_THREADS, 0);
+        if (P.width == NV * VEC * TPR) return ln_launch<T, VEC, NV, TPR, true, true>(o, P);
+    if constexpr (!MOST && NV > 1)
+        if (P.width > (NV - 1) * VEC * TPR) return ln_launch<T, VEC, NV, TPR, WHOLE, true>(o, P);
+    const auto kernel = layer_norm_kernel<T, VEC, NV, TPR, WHOLE, MOST>;
+    static const int64_t cap = resident(o, kernel, LN_THREADS, 0);
     const int64_t want = ceil_div(P.rows, LN_THREADS / TPR);
-    return launch(o, layer_norm_kernel<T, VEC, NV, TPR, WHOLE>, dim3(unsigned(want < cap ? want : cap)), LN_THREADS, 0, P);
+    return launch(o, kernel, dim3(unsigned(want < cap ? want : cap)), LN_THREADS, 0, P);
 }
 // A warp takes a row of up to 32 elements a lane, without a barrier; wider rows take a block.
 template <typename T, int VEC>
@@ -154,9 +157,11 @@ constexpr int LN_MOST_WIDTH = 8192;
 // blocks to a column of the long rows' column sums
 int64_t ln_wide_groups(const scalecom_ops* o, int64_t width) { return ceil_div(int64_t(o->sms) * 8, ceil_div(width, LN_THREADS)); }
 
-template <typename T, int VEC, int NV, int TPR, bool DW>
+template <typename T, int VEC, int NV, int TPR, bool DW, bool MOST = false>
 cudaError_t ln_launch_backward_dw(scalecom_ops* o, LnParams& P) {
-    const auto kernel = layer_norm_backward_kernel<T, VEC, NV, TPR, DW>;
+    if constexpr (!MOST && NV > 1)
+        if (P.width > (NV - 1) * VEC * TPR) return ln_launch_backward_dw<T, VEC, NV, TPR, DW, true>(o, P);
+    const auto kernel = layer_norm_backward_kernel<T, VEC, NV, TPR, DW, MOST>;
     const size_t smem = DW && TPR == 32 ? size_t(P.width) * 8 * (LN_THREADS / 32) : 0;
     constexpr size_t most = DW && TPR == 32 ? size_t(NV) * VEC * 32 * 8 * (LN_THREADS / 32) : 0;
     static const cudaError_t set = most > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)) : cudaSuccess;
