@@ -86,23 +86,6 @@ __device__ __forceinline__ void store_down(T* p, const float (&v)[N]) {
 
 // 32 consecutive elements of one row: 16-byte accesses where the address and the row's end allow it
 template <typename T>
-__device__ __forceinline__ void store_row32(T* p, const float* v, int ncols) {
-    constexpr int N = 16 / sizeof(T);
-    if (ncols >= 32 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
-#pragma unroll
-        for (int i = 0; i < 32; i += N) {
-            float t[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) t[j] = v[i + j];
-            store_down<T, N>(p + i, t);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < ncols) p[i] = Elem<T>::down(v[i]);
-    }
-}
-template <typename T>
 __device__ __forceinline__ void load_row32(const T* p, float* v, int ncols) {
     constexpr int N = 16 / sizeof(T);
     if (ncols >= 32 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
@@ -122,11 +105,6 @@ __device__ __forceinline__ void load_row32(const T* p, float* v, int ncols) {
 __device__ __forceinline__ float warp_sum_f(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-    return v;
-}
-__device__ __forceinline__ float warp_max_f(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
     return v;
 }
 
