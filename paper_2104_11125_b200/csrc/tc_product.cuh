@@ -416,15 +416,22 @@ template <int NJ> __device__ __forceinline__ int tc_units(const TcParams<NJ>& P)
 struct Ring {
     uint32_t base;
     int n;
+    bool whole;               // the last block was of 32 bits: it took the whole ring, as one group
 };
 __device__ __forceinline__ uint32_t piece16(uint32_t row, uint32_t piece) { return row * 64u + ((piece ^ ((row >> 1) & 3u)) << 4); }
 __device__ __forceinline__ uint32_t piece32(uint32_t row, uint32_t piece) { return row * 128u + ((piece ^ (row & 7u)) << 4); }
 
-// the next free block of the ring; at most its own size in blocks are still being read by the stores issued before
+// The next free block of the ring. Two blocks of 16 bits fit, so one store may still be reading when the next block is laid out. A block of
+// 32 bits takes all of it: it waits for every store before it, and a block of 16 bits behind it waits for it (a launch of
+// several products may have outputs of both sizes).
 template <int BYTES>
 __device__ __forceinline__ uint32_t ring_next(Ring& r) {
     constexpr int SLOTS = BYTES == 2 ? 2 : 1;
-    if (lane_id() == 0) bulk_wait_read<SLOTS - 1>();
+    if (lane_id() == 0) {
+        if (BYTES == 2 && !r.whole) bulk_wait_read<1>();
+        else bulk_wait_read<0>();
+    }
+    r.whole = BYTES == 4;
     __syncwarp();
     return r.base + uint32_t(r.n++ & (SLOTS - 1)) * (TC_RING / SLOTS);
 }
@@ -862,7 +869,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
         uint32_t top = 0u, top2 = 0u;
         int n_acc = 0;
         const uint32_t stage0 = tiles0 + S::STAGES * S::STAGE_BYTES;
-        Ring ring = {stage0 + (warp - 4u) * S::RING, 0};
+        Ring ring = {stage0 + (warp - 4u) * S::RING, 0, false};
         Inflow in = {stage0 + TC_EPI_WARPS * S::RING + (warp - 4u) * S::IN_BYTES, inflow0 + 8u * (warp - 4u), 0u, false};
         auto begin = [&](const TcUnit& u, int row0, int c) {
             if (S::LOADS && c < CHUNKS) inflow_start<EPI>(P.job[NJ > 1 ? u.job : 0], P.more, in, row0, u.nt * WIDTH + chunk(c), u.batch);

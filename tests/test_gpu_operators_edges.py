@@ -1,0 +1,62 @@
+"""The learner-side operators where one of their parts meets another: launches of several products, values at the edges of what a
+type or a scale holds, arguments that share memory."""
+import math
+
+import pytest
+import torch
+
+import paper_2104_11125_b200 as sc
+from paper_2104_11125_b200 import binding as b
+from tests import operator_bounds as ob
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+KINDS = [torch.float32, torch.float16, torch.bfloat16]
+IDS = ["f32", "f16", "bf16"]
+kinds = pytest.mark.parametrize("kind", KINDS, ids=IDS)
+
+
+@pytest.fixture(scope="module")
+def ops():
+    with sc.Operators() as o:
+        yield o
+        assert o.status() == 0
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+# ---- gated feed-forward block ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", KINDS[1:], ids=IDS[1:])
+@pytest.mark.parametrize("t,d,f", [(8192, 1024, 128), (16384, 512, 128), (16384, 520, 72)])
+def test_outputs_of_both_sizes_in_one_launch(ops, kind, t, d, f):
+    """16-bit activations with fp32 weight gradients and more tokens than twice the hidden size: the gradients' products, whose
+    sums over the tokens are the longest, come before dx in one launch, so the same warps store blocks of 32 bits and then of 16.
+    The launch with 16-bit gradients sums in the same order and stores blocks of one size: dx has to be the same bits, and its
+    gradients the fp32 ones rounded."""
+    g = gen(t + d)
+    x, dy = randn(g, t, d).to(kind), (0.25 * randn(g, t, d)).to(kind)
+    wg, wu = (randn(g, f, d) / math.sqrt(d)).to(kind), (randn(g, f, d) / math.sqrt(d)).to(kind)
+    wd = (randn(g, d, f) / math.sqrt(f)).to(kind)
+    y, saved = torch.empty_like(x), torch.empty(2, t, f, device=DEV, dtype=kind)
+    ops.gated_ffn(x, wg, wu, wd, y, saved=saved)
+
+    def grads(wide):
+        out = [torch.empty_like(x)] + [torch.empty(w.shape, device=DEV, dtype=torch.float32 if wide else kind) for w in (wg, wu, wd)]
+        ops.gated_ffn_backward(dy, x, wg, wu, wd, saved, *out)
+        return out
+    narrow = grads(False)
+    first = grads(True)
+    for again in range(20):
+        wide = first if not again else grads(True)
+        assert torch.equal(wide[0], narrow[0])
+        for p, q, r in zip(wide[1:], narrow[1:], first[1:]):
+            assert torch.equal(p.to(kind), q) and torch.equal(p, r)
