@@ -29,6 +29,10 @@ struct scalecom_ops {
     uint32_t* ctrl = nullptr;           // device: [0] status, [16..] arrival counters of split products
     PFN_cuTensorMapEncodeTiled encode = nullptr;
     bool poisoned = false;
+    // Blocks of a kernel that fit a multiprocessor, looked up once. In the handle, since the answer is its device's.
+    struct Fit { const void* kernel; int blocks; };
+    static constexpr int FITS = 512;            // more than there are layer norm kernels
+    Fit fits[FITS] = {};
 };
 
 namespace {
@@ -110,11 +114,19 @@ constexpr int LN_MOST_BLOCKS = 4;       // of a backward kernel on a multiproces
 
 // blocks of a kernel that fit the device at once
 template <typename K>
-int64_t resident(const scalecom_ops* o, K kernel, int threads, size_t smem, int most = 32) {
-    int per = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, threads, smem) != cudaSuccess || per < 1) per = 1;
-    if (per > most) per = most;
-    return int64_t(o->sms) * per;
+int64_t resident(scalecom_ops* o, K kernel, int threads, size_t smem, int most = 32) {
+    const void* key = reinterpret_cast<const void*>(kernel);
+    size_t at = (reinterpret_cast<uintptr_t>(key) >> 4) % scalecom_ops::FITS;
+    for (int i = 0; i < scalecom_ops::FITS && o->fits[at].kernel && o->fits[at].kernel != key; ++i) at = (at + 1) % scalecom_ops::FITS;
+    int per = o->fits[at].kernel == key ? o->fits[at].blocks : 0;
+    if (!per) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, threads, smem) != cudaSuccess || per < 1) {
+            cudaGetLastError();
+            return o->sms;                      // not kept: the next call asks again
+        }
+        if (!o->fits[at].kernel) o->fits[at] = {key, per};
+    }
+    return int64_t(o->sms) * (per < most ? per : most);
 }
 
 template <typename T, int VEC, int NV, int TPR, bool WHOLE = false, bool MOST = false>
@@ -124,7 +136,7 @@ cudaError_t ln_launch(scalecom_ops* o, const LnParams& P) {
     if constexpr (!MOST && NV > 1)
         if (P.width > (NV - 1) * VEC * TPR) return ln_launch<T, VEC, NV, TPR, WHOLE, true>(o, P);
     const auto kernel = layer_norm_kernel<T, VEC, NV, TPR, WHOLE, MOST>;
-    static const int64_t cap = resident(o, kernel, LN_THREADS, 0);
+    const int64_t cap = resident(o, kernel, LN_THREADS, 0);
     const int64_t want = ceil_div(P.rows, LN_THREADS / TPR);
     return launch(o, kernel, dim3(unsigned(want < cap ? want : cap)), LN_THREADS, 0, P);
 }
@@ -157,16 +169,28 @@ constexpr int LN_MOST_WIDTH = 8192;
 // blocks to a column of the long rows' column sums
 int64_t ln_wide_groups(const scalecom_ops* o, int64_t width) { return ceil_div(int64_t(o->sms) * 8, ceil_div(width, LN_THREADS)); }
 
+// shared memory of a backward kernel at its widest: the sums of a block's warps
+template <int VEC, int NV, int TPR, bool DW> constexpr size_t ln_backward_smem() {
+    return DW && TPR == 32 ? size_t(NV) * VEC * 32 * 8 * (LN_THREADS / 32) : 0;
+}
+// Above 48 KB a device has to be told, once for each: 32 columns a lane.
+template <typename T>
+cudaError_t ln_attributes() {
+    constexpr int V = 16 / sizeof(T), NV = 32 / V;
+    constexpr int most = int(ln_backward_smem<V, NV, 32, true>());
+    const cudaError_t e = cudaFuncSetAttribute(layer_norm_backward_kernel<T, V, NV, 32, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(layer_norm_backward_kernel<T, V, NV, 32, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+}
+
 template <typename T, int VEC, int NV, int TPR, bool DW, bool MOST = false>
 cudaError_t ln_launch_backward_dw(scalecom_ops* o, LnParams& P) {
     if constexpr (!MOST && NV > 1)
         if (P.width > (NV - 1) * VEC * TPR) return ln_launch_backward_dw<T, VEC, NV, TPR, DW, true>(o, P);
     const auto kernel = layer_norm_backward_kernel<T, VEC, NV, TPR, DW, MOST>;
     const size_t smem = DW && TPR == 32 ? size_t(P.width) * 8 * (LN_THREADS / 32) : 0;
-    constexpr size_t most = DW && TPR == 32 ? size_t(NV) * VEC * 32 * 8 * (LN_THREADS / 32) : 0;
-    static const cudaError_t set = most > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)) : cudaSuccess;
-    if (set != cudaSuccess) return set;
-    static const int64_t fit = resident(o, kernel, LN_THREADS, most, LN_MOST_BLOCKS);
+    constexpr size_t most = ln_backward_smem<VEC, NV, TPR, DW>();
+    static_assert(most <= 48 * 1024 || NV * VEC == 32, "set in ln_attributes");
+    const int64_t fit = resident(o, kernel, LN_THREADS, most, LN_MOST_BLOCKS);
     int64_t blocks = ceil_div(P.rows, LN_THREADS / TPR);
     if (blocks > fit) blocks = fit;
     // each block leaves a partial sum that is written and read again: at most an eighth of the rows' own traffic
@@ -941,6 +965,9 @@ int scalecom_ops_create(scalecom_ops** out) {
         if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !fn)) e = cudaErrorSymbolNotFound;
         o->encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled>(fn);
     }
+    if (e == cudaSuccess) e = ln_attributes<float>();
+    if (e == cudaSuccess) e = ln_attributes<__half>();
+    if (e == cudaSuccess) e = ln_attributes<__nv_bfloat16>();
     if (e == cudaSuccess) e = tc_attributes<EPI_STORE>();
     if (e == cudaSuccess) e = tc_attribute<256, EPI_STORE, 1, 2, TC_JOBS>();
     if (e == cudaSuccess) e = tc_attribute<256, EPI_STORE, 2, 2, TC_JOBS>();
