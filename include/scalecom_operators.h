@@ -56,7 +56,8 @@ typedef struct scalecom_ops scalecom_ops;
 
 /*
  * Operator handle on the current device: a stream binding (default: the legacy
- * default stream) and scratch memory.  Holds no state between calls.
+ * default stream) and scratch memory.  Holds no state between calls.  Every DEVICE
+ * pointer of its calls is one that this device can read, or write, itself.
  * Errors: NULL_PTR, ALLOC, CUDA (also: not a compute capability 10.0 device).
  */
 int scalecom_ops_create(scalecom_ops** out);

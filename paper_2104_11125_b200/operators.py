@@ -60,17 +60,19 @@ def _check(rc: int, where: str) -> None:
         raise ScaleComError(rc, where)
 
 
-def _type(t: torch.Tensor, name: str) -> int:
+# dev: the index of the handle's device. A kernel reads what it is given from there, so a tensor of another device (or of the host)
+# is refused here; get_device() is -1 for the host's.
+def _type(dev: int, t: torch.Tensor, name: str) -> int:
     kind = TYPES.get(t.dtype)
-    if kind is None or not t.is_cuda:
-        raise TypeError("%s must be a CUDA tensor of float32, float16 or bfloat16" % name)
+    if kind is None or t.get_device() != dev:
+        raise TypeError("%s must be a tensor of float32, float16 or bfloat16 on the handle's device cuda:%s" % (name, dev))
     return kind
 
 
-def _matrix(t: torch.Tensor, kind: torch.dtype, shape: torch.Size, name: str) -> int:
+def _matrix(dev: int, t: torch.Tensor, kind: torch.dtype, shape: torch.Size, name: str) -> int:
     """Row distance of a matrix whose rows are contiguous (a slice of longer rows is fine)."""
-    if t.dtype is not kind or not t.is_cuda:
-        raise TypeError("%s must be a CUDA tensor of %s" % (name, kind))
+    if t.dtype is not kind or t.get_device() != dev:
+        raise TypeError("%s must be a tensor of %s on the handle's device cuda:%s" % (name, kind, dev))
     if t.shape != shape or len(shape) != 2:
         raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
     s0, s1 = t.stride()
@@ -80,31 +82,38 @@ def _matrix(t: torch.Tensor, kind: torch.dtype, shape: torch.Size, name: str) ->
     return s0 if s0 >= cols else cols
 
 
-def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+def _vector(dev: int, t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype is torch.float32 and t.numel() == n and t.is_contiguous()):
-        raise TypeError("%s must be a contiguous CUDA float32 tensor of %d elements" % (name, n))
+    if not (t.get_device() == dev and t.dtype is torch.float32 and t.numel() == n and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous float32 tensor of %d elements on the handle's device cuda:%s" % (name, n, dev))
     return t.data_ptr()
 
 
-def _whole(t: Optional[torch.Tensor], kinds: Sequence[torch.dtype], shape, name: str) -> Optional[int]:
+def _whole(dev: int, t: Optional[torch.Tensor], kinds: Sequence[torch.dtype], shape, name: str) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype not in kinds or not t.is_cuda or not t.is_contiguous():
-        raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, " or ".join(map(str, kinds))))
+    if t.dtype not in kinds or t.get_device() != dev or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous tensor of %s on the handle's device cuda:%s" % (name, " or ".join(map(str, kinds)), dev))
     if t.shape != shape:
         raise ValueError("%s must be of shape %s" % (name, shape))
     return t.data_ptr()
 
 
 class Operators:
-    """One operator handle: a stream binding and scratch.  Inputs and outputs belong to the caller."""
+    """One operator handle on the current device: a stream binding and scratch.  Inputs and outputs belong to the caller.
+
+    Tensors have to be on the handle's device.  Calls run on the stream that the handle is bound to -- by default the legacy default
+    stream, which is also torch's default one -- and not on the stream that is current where they are made: inside
+    `with torch.cuda.stream(s)` bind the handle to s, or order the two streams with events."""
+
+    _device: Optional[int] = None
 
     def __init__(self, stream: Optional[torch.cuda.Stream] = None):
         h, L = ctypes.c_void_p(), lib()
         _check(L.scalecom_ops_create(ctypes.byref(h)), "scalecom_ops_create")
         self._h = h.value
+        self._device = torch.cuda.current_device()
         # looked up once: a small call's time is its way through here
         self._layer_norm, self._layer_norm_backward = L.scalecom_layer_norm, L.scalecom_layer_norm_backward
         self._gated_ffn, self._gated_ffn_backward = L.scalecom_gated_ffn, L.scalecom_gated_ffn_backward
@@ -147,47 +156,47 @@ class Operators:
     def layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,
                    mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None) -> None:
         """y = (x - mean) * rstd * gamma + beta over the last dimension of the matrix x."""
-        kind, shape = x.dtype, x.shape
-        code = _type(x, "x")
+        dev, kind, shape = self._device, x.dtype, x.shape
+        code = _type(dev, x, "x")
         rows, width = shape
-        _check(self._layer_norm(self._h, code, rows, width, x.data_ptr(), _matrix(x, kind, shape, "x"),
-                                         _vector(gamma, width, "gamma"), _vector(beta, width, "beta"), eps,
-                                         y.data_ptr(), _matrix(y, kind, shape, "y"),
-                                         _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd")), "scalecom_layer_norm")
+        _check(self._layer_norm(self._h, code, rows, width, x.data_ptr(), _matrix(dev, x, kind, shape, "x"),
+                                         _vector(dev, gamma, width, "gamma"), _vector(dev, beta, width, "beta"), eps,
+                                         y.data_ptr(), _matrix(dev, y, kind, shape, "y"),
+                                         _vector(dev, mean, rows, "mean"), _vector(dev, rstd, rows, "rstd")), "scalecom_layer_norm")
 
     def layer_norm_backward(self, dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
                             dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
                             dbeta: Optional[torch.Tensor] = None) -> None:
         """dx, and the gradients of gamma and beta (written, not added to)."""
-        kind, shape = x.dtype, x.shape
-        code = _type(x, "x")
+        dev, kind, shape = self._device, x.dtype, x.shape
+        code = _type(dev, x, "x")
         rows, width = shape
         _check(self._layer_norm_backward(
-            self._h, code, rows, width, dy.data_ptr(), _matrix(dy, kind, shape, "dy"),
-            x.data_ptr(), _matrix(x, kind, shape, "x"), _vector(gamma, width, "gamma"),
-            _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
-            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dx, kind, shape, "dx"),
-            _vector(dgamma, width, "dgamma"), _vector(dbeta, width, "dbeta")), "scalecom_layer_norm_backward")
+            self._h, code, rows, width, dy.data_ptr(), _matrix(dev, dy, kind, shape, "dy"),
+            x.data_ptr(), _matrix(dev, x, kind, shape, "x"), _vector(dev, gamma, width, "gamma"),
+            _vector(dev, mean, rows, "mean"), _vector(dev, rstd, rows, "rstd"),
+            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dev, dx, kind, shape, "dx"),
+            _vector(dev, dgamma, width, "dgamma"), _vector(dev, dbeta, width, "dbeta")), "scalecom_layer_norm_backward")
 
     def gated_ffn(self, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, y: torch.Tensor,
                   saved: Optional[torch.Tensor] = None, activation: str = "silu") -> None:
         """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; saved [2, tokens, hidden] keeps what the backward pass needs."""
-        kind, shape = x.dtype, x.shape
-        code = _type(x, "x")
+        dev, kind, shape = self._device, x.dtype, x.shape
+        code = _type(dev, x, "x")
         (tokens, width), hidden, k = shape, w_gate.shape[0], (kind,)
         _check(self._gated_ffn(
-            self._h, code, ACTIVATIONS[activation], tokens, width, hidden, x.data_ptr(), _matrix(x, kind, shape, "x"),
-            _whole(w_gate, k, (hidden, width), "w_gate"), _whole(w_up, k, (hidden, width), "w_up"),
-            _whole(w_down, k, (width, hidden), "w_down"), y.data_ptr(), _matrix(y, kind, shape, "y"),
-            _whole(saved, k, (2, tokens, hidden), "saved")), "scalecom_gated_ffn")
+            self._h, code, ACTIVATIONS[activation], tokens, width, hidden, x.data_ptr(), _matrix(dev, x, kind, shape, "x"),
+            _whole(dev, w_gate, k, (hidden, width), "w_gate"), _whole(dev, w_up, k, (hidden, width), "w_up"),
+            _whole(dev, w_down, k, (width, hidden), "w_down"), y.data_ptr(), _matrix(dev, y, kind, shape, "y"),
+            _whole(dev, saved, k, (2, tokens, hidden), "saved")), "scalecom_gated_ffn")
 
     def gated_ffn_backward(self, dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
                            saved: torch.Tensor, dx: Optional[torch.Tensor] = None, dw_gate: Optional[torch.Tensor] = None,
                            dw_up: Optional[torch.Tensor] = None, dw_down: Optional[torch.Tensor] = None,
                            activation: str = "silu") -> None:
         """Gradients of the block (written, not added to); the weights' may be float32 whatever the type of x."""
-        kind, shape = x.dtype, x.shape
-        code = _type(x, "x")
+        dev, kind, shape = self._device, x.dtype, x.shape
+        code = _type(dev, x, "x")
         (tokens, width), hidden, k = shape, w_gate.shape[0], (kind,)
         grads = [g for g in (dw_gate, dw_up, dw_down) if g is not None]
         gk = (grads[0].dtype if grads else kind,)
@@ -195,12 +204,12 @@ class Operators:
             raise TypeError("weight gradients must be of x's type or float32")
         _check(self._gated_ffn_backward(
             self._h, code, TYPES[gk[0]], ACTIVATIONS[activation], tokens, width, hidden,
-            dy.data_ptr(), _matrix(dy, kind, shape, "dy"), x.data_ptr(), _matrix(x, kind, shape, "x"),
-            _whole(w_gate, k, (hidden, width), "w_gate"), _whole(w_up, k, (hidden, width), "w_up"),
-            _whole(w_down, k, (width, hidden), "w_down"), _whole(saved, k, (2, tokens, hidden), "saved"),
-            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dx, kind, shape, "dx"),
-            _whole(dw_gate, gk, (hidden, width), "dw_gate"), _whole(dw_up, gk, (hidden, width), "dw_up"),
-            _whole(dw_down, gk, (width, hidden), "dw_down")), "scalecom_gated_ffn_backward")
+            dy.data_ptr(), _matrix(dev, dy, kind, shape, "dy"), x.data_ptr(), _matrix(dev, x, kind, shape, "x"),
+            _whole(dev, w_gate, k, (hidden, width), "w_gate"), _whole(dev, w_up, k, (hidden, width), "w_up"),
+            _whole(dev, w_down, k, (width, hidden), "w_down"), _whole(dev, saved, k, (2, tokens, hidden), "saved"),
+            None if dx is None else dx.data_ptr(), width if dx is None else _matrix(dev, dx, kind, shape, "dx"),
+            _whole(dev, dw_gate, gk, (hidden, width), "dw_gate"), _whole(dev, dw_up, gk, (hidden, width), "dw_up"),
+            _whole(dev, dw_down, gk, (width, hidden), "dw_down")), "scalecom_gated_ffn_backward")
 
     def orthogonalise(self, update: torch.Tensor, out: torch.Tensor, steps: int = 5,
                       coefficients: Sequence = (3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0) -> None:
@@ -208,7 +217,8 @@ class Operators:
         coefficients: (a, b, c), or one such triple for each step."""
         if update.dim() not in (2, 3) or out.shape != update.shape:
             raise ValueError("update and out must be matrices, or batches of matrices, of one shape")
-        kin, kout = _type(update, "update"), _type(out, "out")
+        dev = self._device
+        kin, kout = _type(dev, update, "update"), _type(dev, out, "out")
         a, b = (update, out) if update.dim() == 3 else (update.unsqueeze(0), out.unsqueeze(0))
         batch, rows, cols = a.shape
         ld, stride = [], []
