@@ -83,7 +83,7 @@ int scalecom_ops_reset(scalecom_ops* ops);
  *   y           may be x itself with the same row distance.
  *   mean, rstd  DEVICE fp32[rows], written; NULL (each) if not wanted.
  * rows = 0 is accepted (nothing is done); width >= 1.  eps >= 0, finite.
- * A row of equal values gives y = beta (with eps > 0); NaN and infinities stay in their row.
+ * A row of equal values gives y = beta (with eps > 0, and its sum within fp32's range); NaN and infinities stay in their row.
  */
 int scalecom_layer_norm(scalecom_ops* ops, int32_t dtype, int64_t rows, int64_t width,
                         const void* x, int64_t ldx, const float* gamma, const float* beta, float eps,

@@ -60,3 +60,26 @@ def test_outputs_of_both_sizes_in_one_launch(ops, kind, t, d, f):
         assert torch.equal(wide[0], narrow[0])
         for p, q, r in zip(wide[1:], narrow[1:], first[1:]):
             assert torch.equal(p.to(kind), q) and torch.equal(p, r)
+
+
+# ---- layer norm ------------------------------------------------------------------------------------------------
+@kinds
+@pytest.mark.parametrize("width", [1, 2, 7, 13, 26, 49, 96, 128, 255, 300, 1001, 1024, 2047, 2048, 4096, 5000, 8192, 9000])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_rows_of_equal_values_give_beta(ops, kind, width, shift):
+    """Of any width, on the 16-byte grid and off it: the mean is the value itself, and 1 / sqrt(eps) has nothing to magnify."""
+    values = torch.tensor([1.0, 3.0, 1000.0, 1000.1, -0.3, 7e-6, 6.1e4, 0.0], device=DEV).to(kind)
+    rows = len(values)
+    flat = torch.empty(shift + rows * width, device=DEV, dtype=kind)
+    x = flat[shift:].view(rows, width)
+    x.copy_(values[:, None].expand(rows, width))
+    g = gen(width)
+    gamma, beta = 1 + 0.1 * randn(g, width), randn(g, width)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    ops.layer_norm(x, gamma, beta, 1e-5, y, mean, rstd)
+    assert torch.equal(mean, values.float())
+    assert torch.equal(y, beta.to(kind).expand(rows, width))
+    # Of the squares there is left what two sums of the first mean's errors squared (50 units in the last place, for 32 terms one after another
+    # and a tree) differ by in rounding; four units in the last place are the root's.
+    left = 2.0 ** -22 * (50 * 2.0 ** -23 * values.double()).square()
+    assert ((rstd.double() * math.sqrt(1e-5) - 1).abs() <= 2.0 ** -22 + 2.0 ** -24 + 0.5 * left / 1e-5).all()
