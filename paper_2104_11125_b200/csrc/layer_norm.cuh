@@ -41,15 +41,16 @@ __device__ __forceinline__ LnMoments ln_merge(const LnMoments& a, const LnMoment
 }
 
 // Mean and squared differences over the TPR threads of a row (32: a warp, LN_THREADS: the block) from those of each thread's N
-// values: pairs of sets of one size, so the pairwise form has constants only. The same bits in every thread. `part`
-// has two arrays used in turn, so that one barrier a row is enough.
+// values: pairs of sets of one size, so the pairwise form has constants only. Either partner of a join computes the same sums of the same
+// two terms, so every thread of the row gets the same bits. `part` has two arrays used in turn, so that one barrier a row is enough.
 template <int TPR, int N>
 __device__ __forceinline__ void row_moments(float& mean, float& m2, float2 (*part)[LN_THREADS / 32], int turn) {
     static_assert(TPR == 32 || TPR == 256, "levels");
     auto join = [&](int o, float size) {
-        const float d = __shfl_xor_sync(FULL, mean, o) - mean;
-        mean += 0.5f * d;
-        m2 += __shfl_xor_sync(FULL, m2, o) + d * d * (0.5f * size);
+        const float other = __shfl_xor_sync(FULL, mean, o), d = other - mean;
+        mean = 0.5f * (mean + other);
+        const float both = m2 + __shfl_xor_sync(FULL, m2, o);
+        m2 = both + d * d * (0.5f * size);
     };
 #pragma unroll
     for (int l = 0; l < 5; ++l) join(1 << l, float(N << l));

@@ -83,3 +83,22 @@ def test_rows_of_equal_values_give_beta(ops, kind, width, shift):
     # and a tree) differ by in rounding; four units in the last place are the root's.
     left = 2.0 ** -22 * (50 * 2.0 ** -23 * values.double()).square()
     assert ((rstd.double() * math.sqrt(1e-5) - 1).abs() <= 2.0 ** -22 + 2.0 ** -24 + 0.5 * left / 1e-5).all()
+
+
+@kinds
+@pytest.mark.parametrize("width", [128, 256, 512, 1024, 2048, 4096, 8192, 100, 1000, 5001, 9000])
+def test_equal_values_of_a_row_stay_equal(ops, kind, width):
+    """A row has one mean and one rstd: columns of one value give one result, whichever thread works on them, and the statistics that are
+    stored are the ones that were used."""
+    g = gen(width)
+    table = randn(g, 16).to(kind)
+    pick = torch.randint(0, 16, (6, width), generator=g, device=DEV)
+    x = table[pick]
+    y, mean, rstd = torch.empty_like(x), torch.empty(6, device=DEV), torch.empty(6, device=DEV)
+    ops.layer_norm(x, None, None, 1e-5, y, mean, rstd)
+    for r in range(6):
+        for v in range(16):
+            got = y[r][pick[r] == v]
+            assert (got == got[:1]).all(), (r, v)
+    # (x - mean) * rstd + 0 in fp32: two roundings, the same here
+    assert torch.equal(y, ((x.float() - mean[:, None]) * rstd[:, None]).to(kind))
