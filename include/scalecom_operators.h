@@ -146,7 +146,9 @@ int scalecom_gated_ffn_backward(scalecom_ops* ops, int32_t dtype, int32_t wgrad_
  *   coefficients    HOST float[3 * ncoef]; ncoef is 1 (the same in every step) or steps.  |.| <= 63 each.
  * Precision follows the output: 16-bit outputs iterate on fp16 values of the power-of-two scaled X and A with fp32
  * accumulation (bf16 iterates would lose the small singular values); fp32 outputs iterate on pairs of fp16 planes,
- * three products each, at fp32's accuracy.
+ * three products each, at fp32's accuracy.  Entries of the normalised X are held to 2^-35 at best: a G whose norm is far
+ * below eps gives an X that much smaller than 1, and keeps fewer bits.  The scales follow the coefficients: whichever are
+ * accepted, results are finite as long as no entry of an X, of its A and of aI + bA + cAA passes 2^75.
  * steps = 0 gives scale * G / (|G|_F + eps).  A zero matrix gives zeros (eps > 0); a NaN or an infinity makes NaN of
  * its own matrix only.  batch = 0 is accepted; rows, cols >= 1; steps <= 64; eps >= 0 and finite; scale finite.
  */

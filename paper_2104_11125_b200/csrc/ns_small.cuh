@@ -11,7 +11,7 @@
 // matrix, with the operands' way through TMEM and back between dependent steps. Their rate is what bounds the kernel (measured:
 // some 20 cycles for 16 x 8 x 16 on a quarter of an SM, whatever is fetched ahead), so a single matrix is shared by a cluster
 // as soon as that is worth its two barriers a step.
-// Values are held as 2^10 times themselves in one or two fp16 planes, as in the large path.
+// Values are held as a power of two times themselves in one or two fp16 planes, as in the large path.
 #pragma once
 #include "ops_common.cuh"
 #include "tc_product.cuh"
@@ -20,7 +20,10 @@ namespace sc {
 
 constexpr int NSS_THREADS = 512, NSS_WARPS = NSS_THREADS / 32;
 constexpr int NSS_MAX_R = 128, NSS_MAX_STEPS = 64;
-constexpr float NSS_SCALE = 1024.0f;
+constexpr float NSS_SCALE = 1024.0f;         // of the first X
+
+// What a step's products are multiplied by: A from X X^T, B = aI + bA + cAA, the next X (or the result) from B X.
+struct NsStep { float gram, poly_a, poly_b, poly_c, apply; };
 
 struct NsSmallParams {
     const void* in;
@@ -30,9 +33,9 @@ struct NsSmallParams {
     int32_t r, n;                  // short and long side
     int32_t tall;                  // stored [n][r]
     int32_t rp, nc;                // r rounded up to 16; columns of a block, a multiple of 16
-    int32_t steps, ncoef;
-    float eps, scale;
-    float co[3 * NSS_MAX_STEPS];
+    int32_t steps;
+    float eps;
+    NsStep step[NSS_MAX_STEPS];
 };
 
 inline int64_t nss_smem(int planes, int64_t rp, int64_t nc, int cluster) {
@@ -174,6 +177,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
     extern __shared__ __align__(16) uint8_t nss_raw[];
     __shared__ double red[NSS_WARPS];
     __shared__ double part;
+    __shared__ NsStep steps[NSS_MAX_STEPS];       // from the parameters the first reads of each step's cost 0.15 us
     const uint32_t warp = warp_id(), lane = lane_id();
     uint32_t blocks = 1, rank = 0;
     if (CLUSTER) {
@@ -188,6 +192,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
     // element (i, j) of the short-side-first matrix, j counted from this block's first column
     auto where = [&](int i, int j, int64_t ld) { return P.tall ? int64_t(first + j) * ld + i : int64_t(i) * ld + first + j; };
     chain_launch();
+    if (int(threadIdx.x) < P.steps) steps[threadIdx.x] = P.step[threadIdx.x];
     chain_wait();
 
     // |X|^2 in fp64, over the cluster
@@ -269,8 +274,8 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
             }
     };
     for (int step = 0; step < P.steps; ++step) {
-        const float* co = P.co + (P.ncoef > 1 ? 3 * step : 0);
-        const float ca = co[0] * NSS_SCALE, cb = co[1], cc = co[2] / NSS_SCALE;
+        const NsStep by = steps[step];
+        const float ca = by.poly_a, cb = by.poly_b, cc = by.poly_c;
         const bool last = step + 1 == P.steps;
         // A = X X^T
         for (int t = warp; t < tiles; t += NSS_WARPS) {
@@ -284,7 +289,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(G + ((t * 8 + i) * 32 + lane) * 4u), "f"(c[i / 4][i % 4]) : "memory");
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) c[i / 4][i % 4] *= 1.0f / NSS_SCALE;
+                for (int i = 0; i < 8; ++i) c[i / 4][i % 4] *= by.gram;
                 put_tile(A, ti, tj, c);
             }
         }
@@ -311,7 +316,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
                         }
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) c[i / 4][i % 4] *= 1.0f / NSS_SCALE;
+                for (int i = 0; i < 8; ++i) c[i / 4][i % 4] *= by.gram;
                 put_tile(A, ti, tj, c);
             }
             cluster_sync();                                  // the parts are read before the next step overwrites them
@@ -379,12 +384,11 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
                     for (int q = 0; q < 2; ++q) {
                         const int row = ti * 16 + fr + 8 * q, col = j0 + fc + 8 * h;
                         if (!last) {
-                            put2<PL>(X + (row * ldx + col) * 2u, plx, c[h][2 * q] * (1.0f / NSS_SCALE), c[h][2 * q + 1] * (1.0f / NSS_SCALE));
+                            put2<PL>(X + (row * ldx + col) * 2u, plx, c[h][2 * q] * by.apply, c[h][2 * q + 1] * by.apply);
                         } else if (row < r) {
                             const int64_t to = int64_t(blockIdx.y) * P.out_stride;
-                            const float f = P.scale / (NSS_SCALE * NSS_SCALE);
-                            if (col < mine) store_one(P.out_type, P.out, to + where(row, col, P.ld_out), c[h][2 * q] * f);
-                            if (col + 1 < mine) store_one(P.out_type, P.out, to + where(row, col + 1, P.ld_out), c[h][2 * q + 1] * f);
+                            if (col < mine) store_one(P.out_type, P.out, to + where(row, col, P.ld_out), c[h][2 * q] * by.apply);
+                            if (col + 1 < mine) store_one(P.out_type, P.out, to + where(row, col + 1, P.ld_out), c[h][2 * q + 1] * by.apply);
                         }
                     }
             }

@@ -758,9 +758,11 @@ int ffn_backward(scalecom_ops* o, const FfnArgs& A, int wgrad_type, const void* 
 }
 
 // ---- Newton-Schulz -----------------------------------------------------------------------------------------------
-// X, A and bA + cAA + aI are held as 2^10 times themselves in fp16 planes: entries up to 63 fit, and the smallest
-// entries that matter (1 / sqrt(rows * cols) of a normalised matrix) stay far above fp16's subnormals.
-constexpr double NS_SCALE = 1024.0;
+// X, A and B = aI + bA + cAA are held as a power of two times themselves in fp16 planes. The scale is 2^10 -- the smallest
+// entries that matter (1 / sqrt(rows * cols) of a normalised matrix) stay far above fp16's subnormals -- as long as no entry can pass 32. An
+// entry is at most the matrix's largest singular value: 1 at first, and then what the coefficients make of it, which ns_steps
+// follows step by step; where that is more, as with coefficients that add up to more than 32, the scale is the power of two that fits.
+constexpr double NS_SCALE = NSS_SCALE, NS_TOP = 32768.0, NS_LEAST = 0x1p-60;
 
 struct NsArgs {
     int64_t batch, rows, cols;
@@ -772,6 +774,46 @@ struct NsArgs {
     const float* co;
     float eps, scale;
 };
+
+double ns_scale(double bound) {
+    double scale = NS_SCALE;
+    while (scale > NS_LEAST && !(scale * bound <= NS_TOP)) scale *= 0.5;
+    return scale;
+}
+// What the products of each step are multiplied by, from the scales of what they read and write.
+void ns_steps(const NsArgs& A, NsStep* out) {
+    double top = 1.0, sx = NS_SCALE;                     // of X: bound of its singular values, scale
+    for (int i = 0; i < A.steps; ++i) {
+        const float* co = A.co + (A.ncoef > 1 ? 3 * i : 0);
+        const double a = co[0], b = co[1], c = co[2];
+        // roundings may have raised it a little; past 10^30 nothing can be kept in range
+        top = std::fmin(top * 1.01, 1e30);
+        const double end = top * top;
+        auto q = [&](double l) { return std::fabs(a + b * l + c * l * l); };
+        auto p = [&](double l) { return std::sqrt(l) * q(l); };
+        double most_q = std::fmax(q(0.0), q(end)), most_p = p(end);
+        auto turn_q = [&](double l) { if (l > 0.0 && l < end) most_q = std::fmax(most_q, q(l)); };
+        auto turn_p = [&](double l) { if (l > 0.0 && l < end) most_p = std::fmax(most_p, p(l)); };
+        if (c != 0.0) {
+            turn_q(-b / (2.0 * c));                      // q' = b + 2 c l
+            const double d = 9.0 * b * b - 20.0 * a * c; // p' ~ a + 3 b l + 5 c l^2
+            if (d >= 0.0) {
+                turn_p((-3.0 * b + std::sqrt(d)) / (10.0 * c));
+                turn_p((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+            }
+        } else if (b != 0.0) {
+            turn_p(-a / (3.0 * b));
+        }
+        const double sa = ns_scale(end), sb = ns_scale(most_q), next = ns_scale(most_p);
+        out[i].gram = float(sa / (sx * sx));
+        out[i].poly_a = float(a * sb);
+        out[i].poly_b = float(b * sb / sa);
+        out[i].poly_c = float(c * sb / (sa * sa));
+        out[i].apply = float((i + 1 < A.steps ? next : double(A.scale)) / (sb * sx));
+        top = most_p;
+        sx = next;
+    }
+}
 
 // Blocks of a cluster for the one-launch kernel, 0: the separate products are taken. By the least estimated cycles: a product of
 // 16 x 8 x 16 takes 20 on a quarter of an SM, a cluster's barriers and sums some thousands a step; the chain of separate products measured
@@ -811,8 +853,8 @@ int orthogonalise_small(scalecom_ops* o, const NsArgs& A, int planes, int cluste
     P.n = int32_t(P.tall ? A.rows : A.cols);
     P.rp = (P.r + 15) / 16 * 16;
     P.nc = int32_t((ceil_div(P.n, cluster) + 15) / 16 * 16);
-    P.steps = A.steps; P.ncoef = A.ncoef; P.eps = A.eps; P.scale = A.scale;
-    for (int i = 0; i < 3 * A.ncoef; ++i) P.co[i] = A.co[i];
+    P.steps = A.steps; P.eps = A.eps;
+    ns_steps(A, P.step);
     const size_t smem = size_t(nss_smem(planes, P.rp, P.nc, cluster));
     const dim3 grid{unsigned(cluster), unsigned(A.batch)};
     auto go = [&](auto kernel) { return launch_cluster(o, cluster, kernel, grid, NSS_THREADS, smem, P); };
@@ -835,6 +877,8 @@ int orthogonalise(scalecom_ops* o, const NsArgs& A) {
     int64_t nparts = ceil_div(A.rows * A.cols, 1 << 14);
     if (nparts > ceil_div(int64_t(o->sms) * 4, B)) nparts = ceil_div(int64_t(o->sms) * 4, B);
     if (nparts > A.rows) nparts = A.rows;
+    NsStep step[NSS_MAX_STEPS];
+    ns_steps(A, step);
     for (int pass = 0; pass < 2; ++pass) {
         Carver c{pass ? static_cast<char*>(o->ws) : nullptr};
         double* part = c.take<double>(B * nparts);
@@ -906,28 +950,26 @@ int orthogonalise(scalecom_ops* o, const NsArgs& A) {
             return SCALECOM_ERR_CUDA;
         }
         for (int s = 0; s < A.steps; ++s) {
-            const float* co = A.co + (A.ncoef > 1 ? 3 * s : 0);
             const Operand *now = &x[s & 1], *next = &x[(s & 1) ^ 1];
             TcParams<1> P;
             std::memset(&P, 0, sizeof P);
             gram.a = gram.b = now;
-            P.job[0].alpha = float(1.0 / NS_SCALE);
+            P.job[0].alpha = step[s].gram;
             if (!set_out(o, P.job[0], 0, surface(g))) return SCALECOM_ERR_CUDA;
             int rc = run_product(o, EPI_GRAM, gram, P, partial);
             if (rc != SCALECOM_OK) return rc;
             std::memset(&P, 0, sizeof P);
-            P.more.poly_a = float(co[0] * NS_SCALE); P.more.poly_b = co[1]; P.more.poly_c = float(co[2] / NS_SCALE);
+            P.more.poly_a = step[s].poly_a; P.more.poly_b = step[s].poly_b; P.more.poly_c = step[s].poly_c;
             if (!set_in(o, P.more, surface(g)) || !set_out(o, P.job[0], 0, surface(q))) return SCALECOM_ERR_CUDA;
             rc = run_product(o, EPI_POLY, poly, P, partial);
             if (rc != SCALECOM_OK) return rc;
             std::memset(&P, 0, sizeof P);
             (tall ? apply.a : apply.b) = now;
+            P.job[0].alpha = step[s].apply;
             if (s + 1 < A.steps) {
-                P.job[0].alpha = float(1.0 / NS_SCALE);
                 if (!set_out(o, P.job[0], 0, surface(*next))) return SCALECOM_ERR_CUDA;
                 rc = run_product(o, EPI_PLANES, apply, P, partial);
             } else {
-                P.job[0].alpha = float(double(A.scale) / (NS_SCALE * NS_SCALE));
                 P.job[0].type = A.out_type;
                 Surface os;
                 os.p = A.out; os.type = A.out_type; os.rows = A.rows; os.cols = A.cols; os.ld = A.ld_out; os.batch = int(B); os.stride = A.out_stride;

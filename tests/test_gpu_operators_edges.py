@@ -102,3 +102,37 @@ def test_equal_values_of_a_row_stay_equal(ops, kind, width):
             assert (got == got[:1]).all(), (r, v)
     # (x - mean) * rstd + 0 in fp32: two roundings, the same here
     assert torch.equal(y, ((x.float() - mean[:, None]) * rstd[:, None]).to(kind))
+
+
+# ---- orthogonalised update --------------------------------------------------------------------------------------
+@kinds
+@pytest.mark.parametrize("rows,cols", [(24, 40), (40, 24), (140, 200), (200, 140)])
+@pytest.mark.parametrize("co,steps,scale", [((60.0, 10.0, 10.0), 1, 0.25), ((60.0, 10.0, 10.0), 2, 2.0 ** -30), ((63.0, 63.0, 63.0), 1, 1.0),
+                                            ((20.0, 0.0, 0.0), 3, 2.0 ** -8), ((-63.0, 63.0, 0.0), 1, 1.0), ((1.0, -63.0, 63.0), 2, 1.0)])
+def test_large_coefficients(ops, kind, rows, cols, co, steps, scale):
+    """Iterates and polynomials beyond 64, from matrices of one entry, for which every product is one term: X0 is exactly 1. Each step
+    rounds A, B and X once (one fp16 plane 2^-11, two 2^-22) and evaluates B in fp32. Errors of X enter the next one five times, of A twice."""
+    g = torch.zeros(2, rows, cols, device=DEV)
+    g[0, 3, 5] = 0.5
+    g[1, 7, 2] = -4.0
+    out = torch.empty(2, rows, cols, device=DEV, dtype=kind)
+    ops.orthogonalise(g, out, steps=steps, coefficients=co, eps=0.0, scale=scale)
+    want = ob.newton_schulz(g.double(), steps, [co], 0.0, scale)
+    u = 2.0 ** -22 if kind == torch.float32 else 2.0 ** -11
+    tol = sum(5.0 ** i * (4 * u + 2.0 ** -21) for i in range(steps)) + ob.U[kind]
+    ob.check(out, want, tol * want.abs(), "one entry")
+
+
+@kinds
+@pytest.mark.parametrize("rows,cols", [(24, 40), (140, 200)])
+def test_coefficients_of_each_step(ops, kind, rows, cols):
+    """A step that makes the singular values large and one that brings them back: the scale follows them up and down."""
+    co = [(40.0, 0.0, 0.0), (0.025, 0.0, 0.0), (1.875, -1.25, 0.375)]
+    g = randn(gen(rows), 3, rows, cols)
+    out = torch.empty(3, rows, cols, device=DEV, dtype=kind)
+    ops.orthogonalise(g, out, steps=3, coefficients=co)
+    exact = ob.newton_schulz(g.double(), 3, co, 1e-7)
+    # three roundings of X on the way, two of B that matter (multiples of the identity), and the sums'
+    u = 2.0 ** -20 if kind == torch.float32 else 2.0 ** -11
+    off, norm = (out.double() - exact).flatten(1).norm(dim=1), exact.flatten(1).norm(dim=1)
+    assert (off <= (8 * u + 2 * ob.U[kind]) * norm).all(), off / norm
