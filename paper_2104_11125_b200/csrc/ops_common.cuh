@@ -118,14 +118,20 @@ __device__ __forceinline__ void chain_launch() { asm volatile("griddepcontrol.la
 // ---- power-of-two scales of fp32 operands --------------------------------------------------------------
 // A tensor's largest finite magnitude (bits in a device word) gives the scale 2^(14 - e), e its exponent: the
 // scaled values are below 2^15, inside fp16's range with room for rounding up.
-__device__ __forceinline__ float plane_scale(uint32_t amax_bits) {
-    int e = int(amax_bits >> 23) - 127;              // -127 for zero and denormals
-    int s = 14 - e;
-    if (amax_bits == 0u) s = 0;
-    if (s > 126) s = 126;                            // both 2^s and 2^-s are normal numbers
-    return __uint_as_float(uint32_t(s + 127) << 23);
+__device__ __forceinline__ int plane_shift(uint32_t amax_bits) {
+    const int e = int(amax_bits >> 23) - 127;        // -127 for zero and denormals
+    return amax_bits == 0u ? 0 : min(14 - e, 126);   // 126: both 2^s and 2^-s are normal numbers
 }
-__device__ __forceinline__ float plane_unscale(uint32_t amax_bits) { return 1.0f / plane_scale(amax_bits); }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(uint32_t(e + 127) << 23); }      // -126 .. 127
+__device__ __forceinline__ float plane_scale(uint32_t amax_bits) { return power_of_two(plane_shift(amax_bits)); }
+// What takes the scales of two operands out of their product again, 2^-(s + s'), as two factors to be applied one after the other: the
+// exponent reaches from -252 to 226, and a product that fp32 holds must neither pass infinity nor zero on its way. The second is 1 unless
+// the first cannot hold it all.
+struct Unscale { float first, second; };
+__device__ __forceinline__ Unscale plane_unscale(uint32_t amax_a, uint32_t amax_b) {
+    const int e = -plane_shift(amax_a) - plane_shift(amax_b), h = e < -126 || e > 127 ? e / 2 : e;
+    return {power_of_two(h), power_of_two(e - h)};
+}
 
 __device__ __forceinline__ uint32_t finite_bits(float v) {
     const uint32_t b = mag_key(v);

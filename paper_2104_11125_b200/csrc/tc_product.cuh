@@ -610,21 +610,35 @@ __device__ __forceinline__ void inflow_start(const TcJob& J, const TcMore& M, In
     }
 }
 
+// the planes' scales taken out of 32 products
+__device__ __forceinline__ void unscale_row(float (&v)[32], const Unscale& un) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= un.first;
+    if (un.second != 1.0f) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= un.second;
+    }
+}
+
 // ---- epilogues on a block of 32 x 32: v (and w) hold this lane's row --------------------------------------------
 template <int EPI, int PL>
-__device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, const TcUnit& u, int row0, int col0, int col_next, float (&v)[32], float (&w)[32], float un,
+__device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, const TcUnit& u, int row0, int col0, int col_next, float (&v)[32], float (&w)[32], const Unscale& un,
                                             uint32_t& top, uint32_t& top2, Ring& ring, Inflow& in, volatile uint32_t* abort, uint32_t* status) {
     if (!block_used<EPI>(J, row0, col0)) return true;
     const int row = row0 + int(lane_id()), nc = J.n - col0;
     const bool inside = row < J.m;
     if (EPI == EPI_STORE) {
+        if (PL == 2) {
+            unscale_row(v, un);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= un;
+            for (int i = 0; i < 32; ++i) v[i] *= un.first;
+        }
         emit<true>(J, 0, ring, J.type, v, row0, col0, 0, u.batch);
     } else if (EPI == EPI_GATE) {
         if (PL == 2) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) { v[i] *= un; w[i] *= un; }
+            unscale_row(v, un);
+            unscale_row(w, un);
         }
         const bool save = J.out[1].base != nullptr;
         float h[32];
@@ -656,10 +670,7 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
             load_typed(J.type, M.in, at, g, inside ? nc : 0);
             load_typed(J.type, M.in, at + M.in_plane, w, inside ? nc : 0);
         }
-        if (PL == 2) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= un;
-        }
+        if (PL == 2) unscale_row(v, un);
 #define SC_CALL(ACT) gate_back_row<ACT>(g, v, w)
         SC_FOR_ACT(M.act, SC_CALL)
 #undef SC_CALL
@@ -878,8 +889,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
                 const TcJob& J = P.job[NJ > 1 ? u.job : 0];
                 const int iters = J.pairs * J.kblocks;
-            float un_scale = J.alpha;
-            if (J.amax_a) un_scale *= plane_unscale(*J.amax_a) * plane_unscale(*J.amax_b);
+            Unscale un_scale = {J.alpha, 1.0f};
+            if (PL == 2 && J.amax_a) un_scale = plane_unscale(*J.amax_a, *J.amax_b);       // alpha is 1 there
             const int row0 = u.mt * S::BM + int(rank) * TC_BM + int(quad) * 32;
             float v[32], w[32];
             float sum[BN / 64][32];       // PL = 2: this thread's columns, in the order of `column`

@@ -62,6 +62,34 @@ def test_outputs_of_both_sizes_in_one_launch(ops, kind, t, d, f):
             assert torch.equal(p.to(kind), q) and torch.equal(p, r)
 
 
+@pytest.mark.parametrize("ex,ew", [(64, 58), (-60, -62), (-2, 70), (-70, 10)])
+def test_fp32_products_of_far_scales(ops, ex, ew):
+    """Operands whose scales multiply to more, or less, than a fp32 holds, and whose products it holds: sums of 8 powers of two are
+    exact. Rows and columns whose products pass the type's range stand beside them and are left out."""
+    t, d, f = 40, 8, 24
+    x = torch.full((t, d), 2.0 ** ex, device=DEV)
+    wg, wu, wd = torch.full((f, d), 2.0 ** ew, device=DEV), torch.full((f, d), 2.0 ** ew, device=DEV), torch.ones(d, f, device=DEV)
+    if ex > 0:
+        x[0] *= 2.0 ** 36
+        wg[1:] *= 2.0 ** -20
+    y, saved = torch.empty_like(x), torch.empty(2, t, f, device=DEV)
+    ops.gated_ffn(x, wg, wu, wd, y, saved=saved, activation="relu")
+    for got, w in ((saved[0], wg), (saved[1], wu)):
+        want = x.double() @ w.double().t()
+        keep = want < 2.0 ** 128
+        assert keep[1:, 1:].all() and torch.equal(got.double()[keep], want[keep])
+
+
+def test_fp32_gradients_of_far_scales(ops):
+    """dw_down = dy^T h with both around 2^-62: every sum is an exact power of two far above the smallest fp32."""
+    t, d, f = 32, 8, 24
+    x, wg = torch.full((t, d), 2.0 ** -20, device=DEV), torch.full((f, d), 2.0 ** -11, device=DEV)
+    dy, saved = torch.full((t, d), 2.0 ** -68, device=DEV), torch.full((2, t, f), 2.0 ** -28, device=DEV)
+    dwd = torch.empty(d, f, device=DEV)
+    ops.gated_ffn_backward(dy, x, wg, wg.clone(), torch.ones(d, f, device=DEV), saved, None, None, None, dwd, activation="relu")
+    assert (dwd.double() == t * 2.0 ** -124).all()
+
+
 # ---- layer norm ------------------------------------------------------------------------------------------------
 @kinds
 @pytest.mark.parametrize("width", [1, 2, 7, 13, 26, 49, 96, 128, 255, 300, 1001, 1024, 2047, 2048, 4096, 5000, 8192, 9000])
