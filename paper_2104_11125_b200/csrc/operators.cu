@@ -1106,7 +1106,7 @@ int scalecom_layer_norm(scalecom_ops* o, int32_t dtype, int64_t rows, int64_t wi
     if (rows == 0) return SCALECOM_OK;
     if (!x || !y) return SCALECOM_ERR_NULL_PTR;
     if ((x == y && ldx != ldy) || same(y, gamma) || same(y, beta) || same(y, mean) || same(y, rstd) || same(mean, rstd) ||
-        same(x, mean) || same(x, rstd))
+        same(x, mean) || same(x, rstd) || same(gamma, mean) || same(gamma, rstd) || same(beta, mean) || same(beta, rstd))
         return SCALECOM_ERR_ALIAS;
     DeviceGuard guard(o->device);
     if (!guard.ok) return SCALECOM_ERR_CUDA;
@@ -1129,7 +1129,7 @@ int scalecom_layer_norm_backward(scalecom_ops* o, int32_t dtype, int64_t rows, i
         return SCALECOM_ERR_INVALID_ARG;
     DeviceGuard guard(o->device);
     if (!guard.ok) return SCALECOM_ERR_CUDA;
-    if (same(dgamma, dbeta)) return SCALECOM_ERR_ALIAS;
+    if (same(dgamma, dbeta) || same(dgamma, gamma) || same(dbeta, gamma)) return SCALECOM_ERR_ALIAS;     // written without rows, too
     if (rows == 0) {
         if ((dgamma && cudaMemsetAsync(dgamma, 0, size_t(width) * 4, o->stream) != cudaSuccess) ||
             (dbeta && cudaMemsetAsync(dbeta, 0, size_t(width) * 4, o->stream) != cudaSuccess))
@@ -1138,8 +1138,8 @@ int scalecom_layer_norm_backward(scalecom_ops* o, int32_t dtype, int64_t rows, i
     }
     if (!dy || !x || !mean || !rstd) return SCALECOM_ERR_NULL_PTR;
     if (same(dx, x) || (same(dx, dy) && lddx != lddy) || same(dx, gamma) || same(dx, mean) || same(dx, rstd) || same(dx, dgamma) ||
-        same(dx, dbeta) || same(dgamma, dy) || same(dbeta, dy) || same(dgamma, x) || same(dbeta, x) || same(dgamma, gamma) ||
-        same(dbeta, gamma) || same(dgamma, mean) || same(dbeta, mean) || same(dgamma, rstd) || same(dbeta, rstd))
+        same(dx, dbeta) || same(dgamma, dy) || same(dbeta, dy) || same(dgamma, x) || same(dbeta, x) || same(dgamma, mean) ||
+        same(dbeta, mean) || same(dgamma, rstd) || same(dbeta, rstd))
         return SCALECOM_ERR_ALIAS;
     if (!dx && !dgamma && !dbeta) return SCALECOM_OK;
     const bool dw = dgamma || dbeta;
@@ -1194,6 +1194,9 @@ int scalecom_gated_ffn_backward(scalecom_ops* o, int32_t dtype, int32_t wgrad_ty
     for (int i = 0; i < 4; ++i)
         for (int j = 0; j < i; ++j)
             if (same(outs[i], outs[j])) return SCALECOM_ERR_ALIAS;
+    for (const void* p : {w_gate, w_up, w_down})
+        for (void* q : {dw_gate, dw_up, dw_down})                 // written without tokens, too
+            if (same(q, p)) return SCALECOM_ERR_ALIAS;
     if (tokens == 0) {
         for (int i = 1; i < 4; ++i)
             if (outs[i] && cudaMemsetAsync(outs[i], 0, size_t(width) * hidden * type_size(wgrad_type), o->stream) != cudaSuccess)

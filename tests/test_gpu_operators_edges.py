@@ -164,3 +164,21 @@ def test_coefficients_of_each_step(ops, kind, rows, cols):
     u = 2.0 ** -20 if kind == torch.float32 else 2.0 ** -11
     off, norm = (out.double() - exact).flatten(1).norm(dim=1), exact.flatten(1).norm(dim=1)
     assert (off <= (8 * u + 2 * ob.U[kind]) * norm).all(), off / norm
+
+
+# ---- arguments that share memory ---------------------------------------------------------------------------------
+def test_outputs_that_are_parameters_are_refused(ops):
+    """Whatever is written, with no rows or tokens at all too, is none of the parameters; nothing is launched."""
+    L, h = sc.operators.lib(), ops._h
+    bufs = [torch.full((64, 64), 7.0, device=DEV) for _ in range(8)]
+    p, q, r, s, t, u, v, w = [x.data_ptr() for x in bufs]
+    for mean, rstd in ((r, None), (None, r), (s, None), (None, s)):
+        assert L.scalecom_layer_norm(h, 0, 8, 8, p, 8, r, s, 1e-5, q, 8, mean, rstd) == b.ERR_ALIAS
+    for rows in (0, 8):
+        for dg, db in ((r, None), (None, r), (r, s)):
+            assert L.scalecom_layer_norm_backward(h, 0, rows, 8, p, 8, q, 8, r, t, u, None, 8, dg, db) == b.ERR_ALIAS
+    for tokens in (0, 8):
+        for grads in ((r, None, None), (s, None, None), (None, t, None), (None, r, None), (None, None, t), (None, None, s)):
+            assert L.scalecom_gated_ffn_backward(h, 0, 0, 0, tokens, 8, 8, p, 8, q, 8, r, s, t, u, None, 8, *grads) == b.ERR_ALIAS
+    torch.cuda.synchronize()
+    assert all((x == 7.0).all() for x in bufs)
