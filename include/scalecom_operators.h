@@ -21,7 +21,12 @@
  *     the same call on the same inputs gives the same bits.
  *   - Calls are asynchronous on the handle's stream, except that a call whose
  *     scratch is larger than any before it on the handle waits for the stream
- *     and allocates (scalecom_ops_reserve does that ahead of time).
+ *     and allocates (scalecom_ops_reserve does that ahead of time; what a call takes is
+ *     what scalecom_ops_workspace says after it on a new handle).
+ *   - Calls may be captured into a CUDA graph.  One that would have to allocate is then
+ *     refused with BAD_STATE.  A graph replays with the scratch of its capture, which the
+ *     handle keeps, outgrown or not, until it is destroyed: replays have to come before
+ *     that, and stand in line with the handle's other calls.
  *   - Outputs must not overlap inputs or one another unless stated (equality of
  *     base pointers is rejected with ALIAS; partial overlap is undefined).
  *   - Nothing is launched when an argument is rejected.  Sizes of zero that are

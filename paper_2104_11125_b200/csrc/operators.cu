@@ -26,6 +26,9 @@ struct scalecom_ops {
     cudaStream_t stream = nullptr;
     void* ws = nullptr;                 // scratch of the calls, grown on demand
     size_t ws_bytes = 0;
+    bool ws_in_graph = false;           // a call that was captured into a graph has its address
+    struct Kept { void* p; Kept* next; };
+    Kept* kept = nullptr;               // scratch of such graphs that has been outgrown
     uint32_t* ctrl = nullptr;           // device: [0] status, [16..] arrival counters of split products
     PFN_cuTensorMapEncodeTiled encode = nullptr;
     bool poisoned = false;
@@ -59,14 +62,36 @@ inline bool type_ok(int t) { return t == SCALECOM_F32 || t == SCALECOM_F16 || t 
 inline int64_t type_size(int t) { return t == SCALECOM_F32 ? 4 : 2; }
 inline bool dim_ok(int64_t v, int64_t low) { return v >= low && v <= SCALECOM_OPS_MAX_DIM; }
 
+bool capturing(const scalecom_ops* o) {
+    if (!o->stream) return false;               // the legacy default stream cannot be captured
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(o->stream, &status) != cudaSuccess) cudaGetLastError();
+    return status != cudaStreamCaptureStatusNone;
+}
+
+// A graph replays its launches with the scratch they were captured with, so that one lives until the handle goes; and nothing can be
+// waited for or allocated while a stream is captured.
 int ensure_ws(scalecom_ops* o, size_t bytes) {
-    if (bytes <= o->ws_bytes) return SCALECOM_OK;
+    const bool graph = capturing(o);
+    if (bytes <= o->ws_bytes) {
+        if (graph) o->ws_in_graph = true;
+        return SCALECOM_OK;
+    }
+    if (graph) return SCALECOM_ERR_BAD_STATE;
     if (cudaStreamSynchronize(o->stream) != cudaSuccess) return SCALECOM_ERR_CUDA;
-    cudaFree(o->ws);
+    if (o->ws_in_graph) {
+        scalecom_ops::Kept* k = new (std::nothrow) scalecom_ops::Kept{o->ws, o->kept};
+        if (!k) return SCALECOM_ERR_ALLOC;
+        o->kept = k;
+    } else {
+        cudaFree(o->ws);
+    }
     o->ws = nullptr;
     o->ws_bytes = 0;
+    o->ws_in_graph = false;
     if (cudaMalloc(&o->ws, bytes) != cudaSuccess) {
         cudaGetLastError();
+        o->ws = nullptr;
         return SCALECOM_ERR_ALLOC;
     }
     o->ws_bytes = bytes;
@@ -1045,6 +1070,12 @@ void scalecom_ops_destroy(scalecom_ops* o) {
     DeviceGuard guard(o->device);
     cudaStreamSynchronize(o->stream);
     cudaFree(o->ws);
+    while (o->kept) {
+        scalecom_ops::Kept* k = o->kept;
+        o->kept = k->next;
+        cudaFree(k->p);
+        delete k;
+    }
     cudaFree(o->ctrl);
     cudaGetLastError();
     delete o;

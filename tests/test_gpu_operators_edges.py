@@ -182,3 +182,69 @@ def test_outputs_that_are_parameters_are_refused(ops):
             assert L.scalecom_gated_ffn_backward(h, 0, 0, 0, tokens, 8, 8, p, 8, q, 8, r, s, t, u, None, 8, *grads) == b.ERR_ALIAS
     torch.cuda.synchronize()
     assert all((x == 7.0).all() for x in bufs)
+
+
+# ---- CUDA graphs -------------------------------------------------------------------------------------------------
+def _block(o, t, d, f, seed):
+    g = gen(seed)
+    x, dy = randn(g, t, d), randn(g, t, d)
+    w = [randn(g, f, d) / d ** 0.5, randn(g, f, d) / d ** 0.5, randn(g, d, f) / f ** 0.5]
+    y, saved, grads = torch.empty_like(x), torch.empty(2, t, f, device=DEV), [torch.empty_like(v) for v in (x, *w)]
+
+    def call():
+        o.gated_ffn(x, *w, y, saved=saved)
+        o.gated_ffn_backward(dy, x, *w, saved, *grads)
+    return call, [y, saved, *grads]
+
+
+def test_a_graph_keeps_the_scratch_it_was_captured_with():
+    """Calls that need more scratch come between a graph's replays; what is allocated meanwhile is not written over."""
+    s = torch.cuda.Stream()
+    with sc.Operators(stream=s) as o:
+        work, outs = _block(o, 64, 128, 256, 1)
+        torch.cuda.synchronize()
+        work()
+        s.synchronize()
+        want = [v.clone() for v in outs]
+        graphs, held = [], []
+        for t in (64, 300, 1200):                                   # each larger than the one before
+            more, _ = _block(o, t, 128, 256, t)
+            torch.cuda.synchronize()
+            more()
+            s.synchronize()
+            held.append(o.workspace())
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                work()
+            graphs.append(graph)
+        assert held == sorted(held) and held[0] < held[2]
+        fill = [torch.full((1 << 20,), 7.0, device=DEV) for _ in range(64)]
+        for graph in graphs + graphs[::-1]:
+            for v in outs:
+                v.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(v, w) for v, w in zip(outs, want))
+        assert all((v == 7.0).all() for v in fill)
+        assert o.status() == 0
+
+
+def test_scratch_cannot_grow_while_a_stream_is_captured():
+    s = torch.cuda.Stream()
+    with sc.Operators(stream=s) as o:
+        work, outs = _block(o, 64, 128, 256, 1)
+        n = torch.zeros(4, device=DEV)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            n += 1
+            with pytest.raises(sc.ScaleComError) as e:
+                work()
+            n += 1
+        assert e.value.code == b.ERR_BAD_STATE
+        graph.replay()                                              # the capture went on
+        torch.cuda.synchronize()
+        assert (n == 2).all()
+        work()                                                      # and the handle takes calls
+        assert o.status() == 0 and o.workspace() > 0
