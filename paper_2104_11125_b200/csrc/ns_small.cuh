@@ -64,7 +64,9 @@ __device__ __forceinline__ double ld_cluster_f64(uint32_t at) {
 }
 
 // A 16 x 16 tile of P Q^T over k, P and Q row-major planes in shared memory: c[0] columns 0-7, c[1] columns 8-15.
-// Two planes: lo hi, hi lo, hi hi, and every 64 k the accumulators are added to sums with correct rounding.
+// Two planes: lo hi, hi lo, hi hi, and every 16 k the accumulators, which the tensor core cuts, are added to sums with correct rounding.
+// (Every 64 k: 8 x 64 x 256 fp32 3.2e-6 from the exact result where plain fp32 products are 1.4e-6; every 16 k 1.2e-6, 39.3 to 40.0 us
+// for one matrix.)
 template <int PL>
 __device__ __forceinline__ void tile_nt(float (&c)[2][4], uint32_t p, uint32_t pl_p, uint32_t ld_p, uint32_t q, uint32_t pl_q, uint32_t ld_q, int k) {
     const uint32_t lane = lane_id();
@@ -84,21 +86,19 @@ __device__ __forceinline__ void tile_nt(float (&c)[2][4], uint32_t p, uint32_t p
             mma16816(c[1], a, b[2], b[3]);
         }
     } else {
-        for (int k0 = 0; k0 < k; k0 += 64) {
+        for (int kk = 0; kk < k; kk += 16) {
             float s[2][4] = {};
-            for (int kk = k0; kk < k && kk < k0 + 64; kk += 16) {
-                uint32_t a[4], b[4], al[4], bl[4];
-                ldm4(al, at_p + pl_p + kk * 2);
-                ldm4(b, at_q + kk * 2);
-                ldm4(a, at_p + kk * 2);
-                ldm4(bl, at_q + pl_q + kk * 2);
-                mma16816(s[0], al, b[0], b[1]);
-                mma16816(s[1], al, b[2], b[3]);
-                mma16816(s[0], a, bl[0], bl[1]);
-                mma16816(s[1], a, bl[2], bl[3]);
-                mma16816(s[0], a, b[0], b[1]);
-                mma16816(s[1], a, b[2], b[3]);
-            }
+            uint32_t a[4], b[4], al[4], bl[4];
+            ldm4(al, at_p + pl_p + kk * 2);
+            ldm4(b, at_q + kk * 2);
+            ldm4(a, at_p + kk * 2);
+            ldm4(bl, at_q + pl_q + kk * 2);
+            mma16816(s[0], al, b[0], b[1]);
+            mma16816(s[1], al, b[2], b[3]);
+            mma16816(s[0], a, bl[0], bl[1]);
+            mma16816(s[1], a, bl[2], bl[3]);
+            mma16816(s[0], a, b[0], b[1]);
+            mma16816(s[1], a, b[2], b[3]);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll

@@ -166,6 +166,27 @@ def test_coefficients_of_each_step(ops, kind, rows, cols):
     assert (off <= (8 * u + 2 * ob.U[kind]) * norm).all(), off / norm
 
 
+@pytest.mark.parametrize("batch,rows,cols", [(16, 16, 16), (8, 24, 40), (8, 64, 256), (8, 256, 64), (8, 100, 90), (4, 128, 512), (4, 128, 128), (4, 30, 2000),
+                                             (2, 300, 200), (2, 511, 700)])
+def test_fp32_results_have_the_accuracy_of_fp32_products(ops, batch, rows, cols):
+    """Against the same iteration with plain fp32 products: half as much again, and 2^-22 for each of the three matrices of a step that
+    are held in two planes."""
+    g = gen(rows * cols)
+    x = randn(g, batch, rows, cols) * (torch.rand(batch, rows, cols, generator=g, device=DEV) < 0.2)
+    x = x + 0.11 * randn(g, batch, rows, 4) @ randn(g, batch, 4, cols)
+    out = torch.empty_like(x)
+    ops.orthogonalise(x, out)
+    exact = ob.newton_schulz(x.double(), 5, [(3.4445, -4.7750, 2.0315)], 1e-7)
+    before = torch.backends.cuda.matmul.allow_tf32
+    torch.backends.cuda.matmul.allow_tf32 = False
+    try:
+        plain = ob.newton_schulz(x, 5, [(3.4445, -4.7750, 2.0315)], 1e-7)
+    finally:
+        torch.backends.cuda.matmul.allow_tf32 = before
+    norm = exact.norm()
+    assert (out.double() - exact).norm() / norm <= 1.5 * (plain.double() - exact).norm() / norm + 3 * 2.0 ** -22
+
+
 # ---- arguments that share memory ---------------------------------------------------------------------------------
 def test_outputs_that_are_parameters_are_refused(ops):
     """Whatever is written, with no rows or tokens at all too, is none of the parameters; nothing is launched."""
