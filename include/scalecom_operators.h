@@ -117,7 +117,9 @@ int scalecom_layer_norm_backward(scalecom_ops* ops, int32_t dtype, int64_t rows,
  * 16-bit types: products of the type's own values with fp32 accumulation; h (and saved) are rounded to the
  * type once, after the activation.  fp32: every operand is split into two fp16 planes after scaling by a power
  * of two (22 mantissa bits; values under 2^-39 of a tensor's largest magnitude are lost) and three products of planes
- * are accumulated in fp32, which keeps fp32's accuracy; a non-finite value makes NaN of what it reaches.
+ * are accumulated in fp32, which keeps fp32's accuracy; a non-finite operand may make NaN of whatever it is multiplied
+ * into.  (Few tokens are multiplied in fp32 as they are.)  g Phi(g) is formed with 1 + erf: far out on the negative side
+ * the error is some 2^-25 of g, not of the value.
  * tokens = 0 is accepted (nothing is done); width, hidden >= 1.
  */
 int scalecom_gated_ffn(scalecom_ops* ops, int32_t dtype, int32_t act, int64_t tokens, int64_t width, int64_t hidden,
