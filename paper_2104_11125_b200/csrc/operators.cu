@@ -448,8 +448,10 @@ int set_job(scalecom_ops* o, int epi, const Product& p, const Plan& pl, TcJob& J
     // fp32 accumulators; both operands fp16 (0) or bf16 (1); majors; N / 8, M / 16
     J.idesc = (1u << 4) | ((p.bf16 ? 1u : 0u) << 7) | ((p.bf16 ? 1u : 0u) << 10) | ((p.a_mn ? 1u : 0u) << 15) |
               ((p.b_mn ? 1u : 0u) << 16) | (uint32_t(pl.bn / 8) << 17) | (uint32_t(TC_BM * pl.cg / 16) << 24);
-    J.amax_a = p.a->amax;
-    J.amax_b = p.b->amax;
+    J.amax_a[0] = p.a->amax;
+    J.amax_b[0] = p.b->amax;
+    if (p.a2) J.amax_a[1] = p.a2->amax;
+    if (p.b2) J.amax_b[1] = p.b2->amax;
     return SCALECOM_OK;
 }
 
@@ -569,7 +571,7 @@ struct Prep {
 };
 
 // largest-magnitude words of a call's fp32 operands
-enum { AM_X = 0, AM_WGU, AM_WD, AM_DY, AM_H, AM_DGU, AM_WORDS };
+enum { AM_X = 0, AM_WG, AM_WU, AM_WD, AM_DY, AM_H, AM_DG, AM_DU, AM_WORDS };
 
 struct FfnArgs {
     int type, act;
@@ -637,7 +639,7 @@ int ffn_forward(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* s
         uint32_t* am = c.take<uint32_t>(AM_WORDS);
         Prep prep(A.type), prep_h(A.type);
         const Operand x = prep.add(c, A.x, T, d, A.ldx, am + AM_X);
-        const Operand wg = prep.add(c, A.wg, f, d, d, am + AM_WGU), wu = prep.add(c, A.wu, f, d, d, am + AM_WGU);
+        const Operand wg = prep.add(c, A.wg, f, d, d, am + AM_WG), wu = prep.add(c, A.wu, f, d, d, am + AM_WU);
         const Operand wd = prep.add(c, A.wd, d, f, f, am + AM_WD);
         void* h = f32 ? static_cast<void*>(c.take<float>(T * fp)) : static_cast<void*>(c.take<uint16_t>(T * fp));
         Operand ho;
@@ -677,7 +679,7 @@ int ffn_forward(scalecom_ops* o, const FfnArgs& A, void* y, int64_t ldy, void* s
             ok = ok && set_out(o, P.job[0], 1, ss);
         }
         if (!ok) return SCALECOM_ERR_CUDA;
-        P.more.amax_o = f32 ? am + AM_H : nullptr;
+        P.more.amax_o[0] = f32 ? am + AM_H : nullptr;
         rc = run_product(o, EPI_GATE, up, P, partial);
         if (rc == SCALECOM_OK) rc = prep_h.run(o, false);
         if (rc != SCALECOM_OK) return rc;
@@ -706,16 +708,15 @@ int ffn_backward(scalecom_ops* o, const FfnArgs& A, int wgrad_type, const void* 
         Operand x, wg, wu;
         if (dwg || dwu) x = prep.add(c, A.x, T, d, A.ldx, am + AM_X);
         if (dx) {
-            wg = prep.add(c, A.wg, f, d, d, am + AM_WGU);
-            wu = prep.add(c, A.wu, f, d, d, am + AM_WGU);
+            wg = prep.add(c, A.wg, f, d, d, am + AM_WG);
+            wu = prep.add(c, A.wu, f, d, d, am + AM_WU);
         }
         // dg, du and h: [3][tokens][fp] in the call's type
         char* mid = c.take<char>(3 * T * fp * e);
         Operand dg, du, h;
         if (f32) {
-            // dg and du share a scale: their products are summed in one accumulator
-            dg = prep_mid.add(c, mid, T, f, fp, am + AM_DGU);
-            du = prep_mid.add(c, mid ? mid + T * fp * e : nullptr, T, f, fp, am + AM_DGU);
+            dg = prep_mid.add(c, mid, T, f, fp, am + AM_DG);
+            du = prep_mid.add(c, mid ? mid + T * fp * e : nullptr, T, f, fp, am + AM_DU);
             h = prep_mid.add(c, mid ? mid + 2 * T * fp * e : nullptr, T, f, fp, am + AM_H);
         } else {
             dg.rows = T; dg.cols = f; dg.ld = fp;
@@ -758,8 +759,7 @@ int ffn_backward(scalecom_ops* o, const FfnArgs& A, int wgrad_type, const void* 
         ss.p = saved; ss.type = A.type; ss.rows = T; ss.cols = f; ss.ld = f; ss.planes = 2; ss.plane = T * f;
         ms.p = mid; ms.type = A.type; ms.rows = T; ms.cols = f; ms.ld = fp; ms.planes = 3; ms.plane = T * fp;
         if (!set_in(o, P.more, ss) || !set_out(o, P.job[0], 0, ms)) return SCALECOM_ERR_CUDA;
-        P.more.amax_o = f32 ? am + AM_DGU : nullptr;
-        P.more.amax_o2 = f32 ? am + AM_H : nullptr;
+        for (int i = 0; i < 3 && f32; ++i) P.more.amax_o[i] = am + (i == 0 ? AM_DG : i == 1 ? AM_DU : AM_H);
         rc = run_product(o, EPI_GATE_BWD, pdh, P, partial);
         if (rc == SCALECOM_OK) rc = prep_mid.run(o, false);
         if (rc != SCALECOM_OK) return rc;

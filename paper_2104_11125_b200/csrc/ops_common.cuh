@@ -124,12 +124,13 @@ __device__ __forceinline__ int plane_shift(uint32_t amax_bits) {
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(uint32_t(e + 127) << 23); }      // -126 .. 127
 __device__ __forceinline__ float plane_scale(uint32_t amax_bits) { return power_of_two(plane_shift(amax_bits)); }
-// What takes the scales of two operands out of their product again, 2^-(s + s'), as two factors to be applied one after the other: the
-// exponent reaches from -252 to 226, and a product that fp32 holds must neither pass infinity nor zero on its way. The second is 1 unless
-// the first cannot hold it all.
+// 2^e takes the scales of two operands out of their product again: -252 .. 226
+__device__ __forceinline__ int plane_unshift(uint32_t amax_a, uint32_t amax_b) { return -plane_shift(amax_a) - plane_shift(amax_b); }
+// It is applied as two factors, one after the other: a product that fp32 holds must neither pass infinity nor zero on its way. The second
+// is 1 unless the first cannot hold it all.
 struct Unscale { float first, second; };
-__device__ __forceinline__ Unscale plane_unscale(uint32_t amax_a, uint32_t amax_b) {
-    const int e = -plane_shift(amax_a) - plane_shift(amax_b), h = e < -126 || e > 127 ? e / 2 : e;
+__device__ __forceinline__ Unscale plane_unscale(int e) {
+    const int h = e < -126 || e > 127 ? e / 2 : e;
     return {power_of_two(h), power_of_two(e - h)};
 }
 

@@ -82,7 +82,7 @@ struct TcJob {
     uint32_t idesc;
     int32_t type;                             // element type of the outputs and of saved
     float alpha;
-    const uint32_t *amax_a, *amax_b;          // largest magnitudes behind the operands' scales, NULL: unscaled
+    const uint32_t *amax_a[2], *amax_b[2];    // largest magnitudes behind the operands' scales, NULL: unscaled; GATE: b[1] is up's
 };
 constexpr int TC_JOBS = 4;
 // what the epilogues other than STORE read besides
@@ -92,7 +92,7 @@ struct TcMore {
     int64_t in_ld, in_plane, in_batch;
     int32_t in_tma;
     int32_t act;
-    uint32_t *amax_o, *amax_o2;               // fp32 intermediates: their largest magnitude is collected
+    uint32_t *amax_o[3];                      // fp32 intermediates: their largest magnitude is collected (GATE: h; GATE_BWD: dg, du, h)
     float poly_a, poly_b, poly_c;
 };
 template <int NJ> struct TcParams {
@@ -624,7 +624,7 @@ __device__ __forceinline__ void unscale_row(float (&v)[32], const Unscale& un) {
 // ---- epilogues on a block of 32 x 32: v (and w) hold this lane's row --------------------------------------------
 template <int EPI, int PL>
 __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, const TcUnit& u, int row0, int col0, int col_next, float (&v)[32], float (&w)[32], const Unscale& un,
-                                            uint32_t& top, uint32_t& top2, Ring& ring, Inflow& in, volatile uint32_t* abort, uint32_t* status) {
+                                            const Unscale& un_up, uint32_t (&top)[3], Ring& ring, Inflow& in, volatile uint32_t* abort, uint32_t* status) {
     if (!block_used<EPI>(J, row0, col0)) return true;
     const int row = row0 + int(lane_id()), nc = J.n - col0;
     const bool inside = row < J.m;
@@ -639,7 +639,7 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
     } else if (EPI == EPI_GATE) {
         if (PL == 2) {
             unscale_row(v, un);
-            unscale_row(w, un);
+            unscale_row(w, un_up);
         }
         const bool save = J.out[1].base != nullptr;
         float h[32];
@@ -653,7 +653,7 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
                 emit<true>(J, 1, ring, J.type, v, row0, col0, 0, 0);
                 emit<true>(J, 1, ring, J.type, w, row0, col0, 1, 0);
             }
-            top = max(top, row_top(h, inside ? nc : 0));
+            top[0] = max(top[0], row_top(h, inside ? nc : 0));
             emit<true>(J, 0, ring, J.type, h, row0, col0, 0, 0);
         }
     } else if (EPI == EPI_GATE_BWD) {
@@ -676,8 +676,9 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
         SC_FOR_ACT(M.act, SC_CALL)
 #undef SC_CALL
         if (PL == 2) {
-            top = max(top, max(row_top(g, inside ? nc : 0), row_top(w, inside ? nc : 0)));
-            top2 = max(top2, row_top(v, inside ? nc : 0));
+            top[0] = max(top[0], row_top(g, inside ? nc : 0));
+            top[1] = max(top[1], row_top(w, inside ? nc : 0));
+            top[2] = max(top[2], row_top(v, inside ? nc : 0));
         }
         if (PL == 1) {
             emit3(J, ring.base, J.type, row0, col0, 0, 0, g, 0, 1, w, 0, 2, v);
@@ -717,6 +718,15 @@ __device__ __forceinline__ bool tc_epilogue(const TcJob& J, const TcMore& M, con
         emit_planes<PL, true>(J, ring, v, row0, col0, u.batch);
     }
     return true;
+}
+
+// Two products of planes that are summed (dx = dg Wg + du Wu) come in different units, 2^e of their operands' scales. Every tensor has a
+// scale of its own: with one for both weights, up weights of 2^-30 of the gate's size were left 10 bits. The product of the smaller
+// unit goes first, so that its sums are scaled down, never up, when the other's are added. By how much the first job's unit is larger:
+template <int EPI, int PL>
+__device__ __forceinline__ int tc_ahead(const TcJob& J) {
+    if (PL != 2 || EPI != EPI_STORE || J.pairs != 2 || !J.amax_a[0]) return 0;
+    return plane_unshift(*J.amax_a[0], *J.amax_b[0]) - plane_unshift(*J.amax_a[1], *J.amax_b[1]);
 }
 
 // whether `ok` holds for all threads of the epilogue warps (a barrier among them)
@@ -793,10 +803,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 const int m0 = u.mt * S::BM + int(rank) * TC_BM;
                 const int n0 = EPI == EPI_GATE ? u.nt * (BN / 2) : u.nt * BN + int(rank) * (BN / CG);
                 const int ba = J.a_batched ? u.batch : 0, bb = J.b_batched ? u.batch : 0;
+                const int second_first = tc_ahead<EPI, PL>(J) > 0;
                 for (int it = it0; it < it1; ++it, ++n_issued) {
                     const int s = n_issued % S::STAGES, round = n_issued / S::STAGES;
                     if (!mbar_wait(empty(s), (round & 1) ^ 1, abort, P.status)) { ok = false; break; }
-                    const int pair = it >= J.kblocks, k0 = (it - pair * J.kblocks) * TC_BK;
+                    const int part = it >= J.kblocks, pair = part ^ second_first, k0 = (it - part * J.kblocks) * TC_BK;
                     const uint32_t a = tiles0 + s * S::STAGE_BYTES, b = a + PL * TC_A_BYTES;
                     const uint32_t bar = CG == 2 ? in_block(full(s), 0) : full(s);
                     if (rank == 0) mbar_expect(full(s), S::STAGE_BYTES * CG);      // both blocks' copies
@@ -878,7 +889,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             if (rank == 0) mbar_arrive(tempty(i));
             else mbar_arrive_cluster(in_block(tempty(i), 0));
         };
-        uint32_t top = 0u, top2 = 0u;
+        uint32_t top[3] = {0u, 0u, 0u};
         int n_acc = 0;
         const uint32_t stage0 = tiles0 + S::STAGES * S::STAGE_BYTES;
         Ring ring = {stage0 + (warp - 4u) * S::RING, 0, false};
@@ -890,8 +901,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             const TcUnit u = tc_unit<BN, EPI, S::BM>(P, un);
                 const TcJob& J = P.job[NJ > 1 ? u.job : 0];
                 const int iters = J.pairs * J.kblocks;
-            Unscale un_scale = {J.alpha, 1.0f};
-            if (PL == 2 && J.amax_a) un_scale = plane_unscale(*J.amax_a, *J.amax_b);       // alpha is 1 there
+            Unscale un_scale = {J.alpha, 1.0f}, un_up = un_scale;
+            const int ahead = tc_ahead<EPI, PL>(J);
+            if (PL == 2 && J.amax_a[0]) {               // alpha is 1 there
+                un_scale = plane_unscale(plane_unshift(*J.amax_a[0], *J.amax_b[0]) - min(ahead, 0));
+                if (EPI == EPI_GATE) un_up = plane_unscale(plane_unshift(*J.amax_a[0], *J.amax_b[1]));
+            }
             const int row0 = u.mt * S::BM + int(rank) * TC_BM + int(quad) * 32;
             float v[32], w[32];
             float sum[BN / 64][32];       // PL = 2: this thread's columns, in the order of `column`
@@ -909,25 +924,38 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                 for (int c = 0; c < BN / 64; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sum[c][i] = 0.0f;
-                for (int it = it0; it < it1; it += TC_CHUNK, ++n_acc) {
-                    q = n_acc % S::ACCS;
-                    ok = __all_sync(FULL, mbar_wait(tfull(q), (n_acc / S::ACCS) & 1, abort, P.status));
-                    if (!ok) break;
-                    tc_fence_after();
-                    acc = tmem + q * BN + lanes;
+                static_assert(TC_CHUNK == 1, "a chunk is of one product");
+                int it = it0;
+#pragma unroll 1
+                for (int part = 0; part < (EPI == EPI_STORE ? 2 : 1) && ok; ++part) {
+                    const int stop = EPI != EPI_STORE || part || J.kblocks > it1 ? it1 : J.kblocks;
+                    if (part && ahead) {            // the first product's sums to the second's unit (zeros, if these k have none of the first)
+                        const float by = abs(ahead) <= 126 ? power_of_two(-abs(ahead)) : 0.0f;
 #pragma unroll
-                    for (int c = 0; c < BN / 64; c += 2) {
-                        tc_ld32x2(acc + column(c), v, acc + column(c + 1), w);
+                        for (int c = 0; c < BN / 64; ++c)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            sum[c][i] += v[i];
-                            sum[c + 1][i] += w[i];
-                        }
+                            for (int i = 0; i < 32; ++i) sum[c][i] *= by;
                     }
-                    if (it + TC_CHUNK < it1) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) acc_free(q);
+                    for (; it < stop; it += TC_CHUNK, ++n_acc) {
+                        q = n_acc % S::ACCS;
+                        ok = __all_sync(FULL, mbar_wait(tfull(q), (n_acc / S::ACCS) & 1, abort, P.status));
+                        if (!ok) break;
+                        tc_fence_after();
+                        acc = tmem + q * BN + lanes;
+#pragma unroll
+                        for (int c = 0; c < BN / 64; c += 2) {
+                            tc_ld32x2(acc + column(c), v, acc + column(c + 1), w);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                sum[c][i] += v[i];
+                                sum[c + 1][i] += w[i];
+                            }
+                        }
+                        if (it + TC_CHUNK < it1) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) acc_free(q);
+                        }
                     }
                 }
                 // the last accumulator is kept until the epilogue has read the sums from its place
@@ -989,7 +1017,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     gather(at, v);
                     if (EPI == EPI_GATE) gather(BN / 2 + at, w);
                     begin(u, row0, c);
-                    ok = ok && tc_epilogue<EPI, PL>(J, P.more, u, row0, u.nt * WIDTH + at, -1, v, w, un_scale, top, top2, ring, in, abort, P.status);
+                    ok = ok && tc_epilogue<EPI, PL>(J, P.more, u, row0, u.nt * WIDTH + at, -1, v, w, un_scale, un_up, top, ring, in, abort, P.status);
                 }
             } else {
 #pragma unroll 1
@@ -1000,7 +1028,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
                     if (c == CHUNKS - 1) release();
                     if (ok) begin(u, row0, c);
                     ok = ok && tc_epilogue<EPI, PL>(J, P.more, u, row0, u.nt * WIDTH + at, c + 1 < CHUNKS ? u.nt * WIDTH + chunk(c + 1) : -1, v, w, un_scale,
-                                                    top, top2, ring, in, abort, P.status);
+                                                    un_up, top, ring, in, abort, P.status);
                 }
             }
         }
@@ -1009,13 +1037,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) tc_product_kernel(const __grid_
             bulk_wait_read<0>();                    // the staging area is read before the block ends; the writes end with the kernel
         }
         if (PL == 2 && (EPI == EPI_GATE || EPI == EPI_GATE_BWD)) {
-            if (P.more.amax_o) {
-                top = __reduce_max_sync(FULL, top);
-                if (lane == 0 && top) atomicMax(P.more.amax_o, top);
-            }
-            if (P.more.amax_o2) {
-                top2 = __reduce_max_sync(FULL, top2);
-                if (lane == 0 && top2) atomicMax(P.more.amax_o2, top2);
+#pragma unroll
+            for (int i = 0; i < (EPI == EPI_GATE ? 1 : 3); ++i) {
+                const uint32_t t = __reduce_max_sync(FULL, top[i]);
+                if (lane == 0 && t) atomicMax(P.more.amax_o[i], t);
             }
         }
     }

@@ -90,6 +90,28 @@ def test_fp32_gradients_of_far_scales(ops):
     assert (dwd.double() == t * 2.0 ** -124).all()
 
 
+@pytest.mark.parametrize("t,d,f", [(50, 40, 56), (300, 136, 264), (1000, 520, 1030)])
+@pytest.mark.parametrize("name,which", [("silu", "w_up"), ("gelu", "w_up"), ("relu", "w_up"), ("relu", "w_gate")])
+def test_fp32_weights_of_far_sizes(ops, t, d, f, name, which):
+    """The block is linear in w_up, and relu's homogeneous in w_gate: 2^-30 of either goes through all of it exactly. Each tensor keeps its
+    bits whatever its neighbour's size."""
+    g = gen(t + d)
+    x, dy = randn(g, t, d), 0.25 * randn(g, t, d)
+    wg, wu, wd = randn(g, f, d) / math.sqrt(d), randn(g, f, d) / math.sqrt(d), randn(g, d, f) / math.sqrt(f)
+    s = 2.0 ** -30
+    runs = []
+    for a in (1.0, s):
+        wg2, wu2 = (wg, wu * a) if which == "w_up" else (wg * a, wu)
+        y, saved, grads = torch.empty_like(x), torch.empty(2, t, f, device=DEV), [torch.empty_like(v) for v in (x, wg, wu, wd)]
+        ops.gated_ffn(x, wg2, wu2, wd, y, saved=saved, activation=name)
+        ops.gated_ffn_backward(dy, x, wg2, wu2, wd, saved, *grads, activation=name)
+        runs.append([y, saved[0], saved[1], *grads])
+    # y, g, u, dx, dw_gate, dw_up, dw_down; the gradient of the weights that shrank stays
+    small = (1, 0, 1, 1, 1, 0, 1) if which == "w_up" else (1, 1, 0, 1, 0, 1, 1)
+    for p, q, scaled in zip(*runs, small):
+        assert torch.equal(q, p * s if scaled else p)
+
+
 # ---- layer norm ------------------------------------------------------------------------------------------------
 @kinds
 @pytest.mark.parametrize("width", [1, 2, 7, 13, 26, 49, 96, 128, 255, 300, 1001, 1024, 2047, 2048, 4096, 5000, 8192, 9000])
